@@ -13,6 +13,8 @@
  *   - The caller owns every buffer it passes in; the library owns the handle and
  *     everything reachable from it (weights, activation arenas, streams).
  *   - A handle is not thread-safe; ens_predict / ens_bench are synchronous.
+ *   - The operators on device buffers (ens_route .. ens_distill_backward) have no handle: they take
+ *     device pointers and a stream, and return when their kernels are issued.
  *   - All image tensors are NHWC (channels fastest).
  */
 #ifndef ENS_H
@@ -58,7 +60,8 @@ typedef enum {
 enum { ENS_OP_CONV = 1, ENS_OP_DWCONV = 2, ENS_OP_MAXPOOL = 3, ENS_OP_AVGPOOL = 4,
        ENS_OP_GAP = 5, ENS_OP_FC = 6, ENS_OP_SE = 7 };
 enum { ENS_ACT_NONE = 0, ENS_ACT_RELU = 1, ENS_ACT_SILU = 2 };
-enum { ENS_FP32 = 0, ENS_BF16 = 1 };
+enum { ENS_FP32 = 0, ENS_BF16 = 1,
+       ENS_FP16 = 2 /* rows of the operators on device buffers only: members are fp32 or bf16 */ };
 
 typedef struct { int32_t h, w, c; } ens_tensor;
 
@@ -233,8 +236,19 @@ int ens_set_combination(ens_handle* h, int32_t rule, const float* weights);
  * rule still run.  The wall time of such an ens_predict is the system's own overhead. */
 int ens_debug_fake_predictor(ens_handle* h, int32_t on);
 
-/* Last per-member logits of the most recent ens_predict (n x classes fp32, host destination);
- * for tests of single members. */
+/* ens_predict with only the k most probable classes of every image (the lowest class first among equal
+ * ones): index_out n x k, prob_out n x k fp32, on the device or the host as the probabilities of
+ * ens_predict would be (ens_set_io).  1 <= k <= min(classes, 128), ENS_E_UNSUPPORTED beyond 128. */
+int ens_predict_top(ens_handle* h, const float* images, int64_t n, int32_t k, int32_t* index_out, float* prob_out);
+
+/* ens_predict with a combination that each image has for itself: Y[i] = sum_j weights[i, j] *
+ * softmax(logits_{chosen[i, j]}[i]).  chosen (int32) and weights (fp32), n x k, are on the device if
+ * the images are, and come from ens_route or from the caller; a choice outside 0 .. members - 1 is
+ * not there.  All members run; the rule of ens_set_combination stays what it is.  1 <= k <= 64. */
+int ens_predict_routed(ens_handle* h, const float* images, int64_t n, int32_t k, const int32_t* chosen, const float* weights, float* probs_out);
+
+/* Last per-member logits of the most recent ens_predict (n x classes fp32, host or device destination), complete when
+ * the call returns; for tests of single members, and for the operators below. */
 int ens_member_logits(ens_handle* h, int32_t member, int64_t n, float* logits_out);
 
 /* Copies tensor `tensor` of member `member` as worker 0 of that member last computed it
@@ -287,6 +301,107 @@ int ens_debug_rows(ens_handle* h, int32_t on);
 int ens_profile_get(const ens_handle* h, int32_t idx, char* name, int32_t name_len, double* ms,
                     int64_t* launches, double* flop, double* bytes);
 double ens_last_ms(const ens_handle* h);
+
+/* ---- operators on device buffers -------------------------------------------------------------
+ * What stands around an ensemble's answer: a gate that chooses members for each row (ens_route), the
+ * combination of the chosen ones (ens_combine_routed), the best classes of a row (ens_top) and the
+ * loss of a student that learns from them (ens_distill), with the backward passes of those that are
+ * trained.  They need no handle and work on rows of any ensemble, image or position of a text.
+ *
+ * Pointers are DEVICE pointers of the current device; `stream` is the caller's hipStream_t (NULL: the
+ * null stream).  A call checks its arguments, issues its kernels on the stream and returns: nothing is
+ * allocated, copied or waited for, and calls may be captured into a graph.  Calls at the same time need
+ * outputs and workspaces of their own.  Outputs are written completely and may not overlap inputs
+ * unless said.  Results depend on the inputs alone: the same call gives the same bits.
+ *   dtype  ENS_FP32, ENS_BF16 or ENS_FP16: the type of gates, logits and values and of their gradients;
+ *          everything else is fp32 or int32.  Sums, maxima and logarithms are held in fp32 or more, a
+ *          gradient is rounded to dtype once, to nearest even.
+ *   ld     elements between the starts of two rows, at least the row's length; rows need no more
+ *          alignment than their elements
+ * Arrays without an ld are contiguous.  n = 0 does nothing.  ENS_E_INVALID for what no call may say,
+ * ENS_E_UNSUPPORTED beyond the stated limits.
+ */
+enum { ENS_SCORE_SOFTMAX = 0, ENS_SCORE_SIGMOID = 1 };
+typedef struct {
+    int32_t k;             /* members chosen for a row, 1 .. 32                                    */
+    int32_t score;         /* ENS_SCORE_*                                                          */
+    int32_t groups;        /* the members stand in this many groups of neighbours (0: one), 64 at most */
+    int32_t groups_kept;   /* members are chosen from that many of them (0: all)                   */
+    int32_t group_best;    /* a group ranks by the sum of this many best members, 1 or 2 (0: two)  */
+    int32_t renormalise;   /* the chosen members' weights add up to `scale`                        */
+    float   scale;         /* multiplies every weight                                              */
+} ens_route_opts;
+
+/* Routing to members.  s = softmax or sigmoid of a row's gate values; a member ranks by s + bias (bias: one float
+ * a member, for balance, or NULL); groups_kept groups stay, those whose group_best best members have the
+ * largest sum of ranks; the k members of highest rank are chosen, the lowest on equal ranks, in that order.
+ *   chosen   n x k int32;  weights  n x k: scale * s, over the sum of the chosen s when renormalised
+ *   load     int32 for each member, or NULL: the call adds the number of rows that chose it
+ * A gate value of minus infinity or NaN, and a rank that is one, takes the member out of the row;
+ * where fewer than k are left the places behind them hold -1 and weight 0.  Plus infinity counts as the
+ * largest fp32 value.  Members 512 at most.  Ranks that differ by less than fp32 resolves are told apart in 64 bits. */
+int ens_route(const void* gates, int32_t dtype, int64_t ld, int64_t n, int32_t members, const ens_route_opts* opts, const float* bias,
+              int32_t* chosen, float* weights, int32_t* load, void* stream);
+/* Gradient of the gate values from d_weights (n x k), that of the weights; the choice and the bias have none.
+ * d_gates: rows of dtype, ld_d apart, written completely.  opts as given to ens_route (of which k, score,
+ * renormalise and scale count). */
+int ens_route_backward(const void* gates, int32_t dtype, int64_t ld, int64_t n, int32_t members, const ens_route_opts* opts,
+                       const int32_t* chosen, const float* d_weights, void* d_gates, int64_t ld_d, void* stream);
+
+/* Combination with weights of each row: probs[i] = sum_j weights[i, j] * softmax(logits[chosen[i, j]][i]).
+ *   logits   HOST array of `members` device pointers (64 at most), each to n rows of `classes` values, ld apart
+ *   chosen, weights  n x k, k 64 at most; a choice outside the members is not there, one that comes
+ *            twice counts with both weights, and members that a row did not choose are not read
+ *   probs    n x classes fp32;  state  n x k x 2 floats for the backward pass, or NULL
+ * A row of logits that are all minus infinity gives nothing.  Up to 16 777 216 classes. */
+int ens_combine_routed(const void* const* logits, int32_t dtype, int64_t ld, int64_t n, int32_t members, int32_t classes, const int32_t* chosen,
+                       const float* weights, int32_t k, float* probs, float* state, void* stream);
+/* Gradients from d_probs (n x classes) and the state that ens_combine_routed left for the same arguments.
+ *   d_weights  n x k (0 where a choice is not there), or NULL
+ *   d_logits   HOST array of `members` device pointers, each to n rows of dtype, ld_d apart, or NULL for a member
+ *              that does not learn; rows that did not choose the member are zeros.  NULL: no member learns */
+int ens_combine_routed_backward(const void* const* logits, int32_t dtype, int64_t ld, int64_t n, int32_t members, int32_t classes,
+                                const int32_t* chosen, const float* weights, int32_t k, const float* state, const float* d_probs,
+                                float* d_weights, void* const* d_logits, int64_t ld_d, void* stream);
+
+/* The k largest values of each row, 1 <= k <= min(classes, 128), largest first, the lowest class first among equal
+ * ones; NaN ranks below minus infinity.  index, value: n x k.
+ *   ENS_TOP_VALUE        the values as they are
+ *   ENS_TOP_LOG          their natural logarithms (of probabilities: what ens_distill takes)
+ *   ENS_TOP_LOG_SOFTMAX  logarithms of the row's softmax at `temperature` (> 0; not read otherwise); minus
+ *                        infinity in a row that holds nothing else
+ * workspace: ens_top_workspace(...) bytes of device memory, 8-byte aligned, that nothing else uses until the
+ * call's kernels have run (0 bytes: NULL).  ens_top_workspace returns a negative status for sizes that ens_top refuses. */
+enum { ENS_TOP_VALUE = 0, ENS_TOP_LOG = 1, ENS_TOP_LOG_SOFTMAX = 2 };
+int ens_top(const void* values, int32_t dtype, int64_t ld, int64_t n, int32_t classes, int32_t k, int32_t form, float temperature,
+            int32_t* index, float* value, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t ens_top_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype);
+
+/* Distillation from the classes that a teacher kept.  For each row, with p = softmax(logits / temperature):
+ *   index, log_probs   n x k, k 256 at most: kept classes and the logarithms of the teacher's probabilities at
+ *            that temperature.  An entry outside 0 .. classes - 1 is not there; a class that comes twice has
+ *            the sum of its probabilities.
+ *   tail 0   q = softmax of log_probs over the entries;  loss = temperature^2 * sum_c q_c ln(q_c / p_c)
+ *   tail 1   q = exp(log_probs), and what they leave of 1 (if anything) is one class more, which stands for all
+ *            the classes without an entry: loss = temperature^2 * (sum_c q_c ln(q_c / p_c) + q_0 ln(q_0 / p_0)).
+ *            262 144 classes at most.  Where the student gives the other classes nothing (none is left,
+ *            or their logits are minus infinity) the tail counts nothing.
+ * A row with no entry of any probability (tail 0), or whose logits are all minus infinity, has loss and gradient 0.
+ *   loss     n;  state  n x 3 floats for the backward pass
+ *   d_logits rows of dtype, ld_d apart, or NULL: the gradient of sum_i row_weights[i] * loss[i], in the same pass.
+ *            It may be the logits themselves (with the same ld).  row_weights: n, or NULL for ones; a row of
+ *            weight 0 gets zeros whatever its logits.
+ *   workspace  ens_distill_workspace(...) bytes of device memory, 8-byte aligned, that nothing else uses until the
+ *            call's kernels have run (0 bytes: NULL) */
+int ens_distill(const void* logits, int32_t dtype, int64_t ld, int64_t n, int32_t classes, const int32_t* index, const float* log_probs,
+                int32_t k, float temperature, int32_t tail, const float* row_weights, float* loss, float* state, void* d_logits, int64_t ld_d,
+                void* workspace, int64_t workspace_bytes, void* stream);
+int64_t ens_distill_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype);
+/* The gradient by itself, from the state that ens_distill left for the same arguments and d_loss, n floats, that of
+ * the losses (NULL: ones).  d_logits as above. */
+int ens_distill_backward(const void* logits, int32_t dtype, int64_t ld, int64_t n, int32_t classes, const int32_t* index, const float* log_probs,
+                         int32_t k, float temperature, int32_t tail, const float* state, const float* d_loss, void* d_logits, int64_t ld_d,
+                         void* stream);
 
 /* ---- host-only planner (no GPU needed) -------------------------------------------------------
  * The optimizer of section "The allocation optimizer" over an explicit memory model and an

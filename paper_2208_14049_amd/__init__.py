@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libens_mi355x.so")
 
 ENS_OK, ENS_E_INVALID, ENS_E_NOMEM, ENS_E_NOFIT, ENS_E_HIP, ENS_E_NODEVICE, ENS_E_UNSUPPORTED, ENS_E_TOOBIG = 0, -1, -2, -3, -4, -5, -6, -7
-ENS_FP32, ENS_BF16 = 0, 1
+ENS_FP32, ENS_BF16, ENS_FP16 = 0, 1, 2
 ENS_MAX_SLOTS, ENS_MAX_MEMBERS, ENS_MAX_DOMAIN = 16, 64, 16
 
 _OP32 = ("kind", "src", "src_c0", "cin", "dst", "dst_c0", "cout", "kh", "kw", "sh", "sw",
@@ -55,6 +55,10 @@ class EnsStats(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int64) for f in ("recorded", "replayed", "graphs", "handed_out", "copies", "copy_bytes", "chained", "rows")]
 
 
+class EnsRouteOpts(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("k", "score", "groups", "groups_kept", "group_best", "renormalise")] + [("scale", ctypes.c_float)]
+
+
 class EnsPlanOpts(ctypes.Structure):
     _fields_ = [("n_domain", ctypes.c_int32), ("domain", ctypes.c_int32 * ENS_MAX_DOMAIN),
                 ("default_batch", ctypes.c_int32), ("segment_size", ctypes.c_int32),
@@ -80,7 +84,8 @@ EXPORTS = ("ens_load", "ens_free", "ens_set_io", "ens_plan", "ens_set_alloc", "e
            "ens_member_logits", "ens_debug_tensor", "ens_debug_keep_tensors", "ens_classes", "ens_n_members", "ens_member_bytes",
            "ens_spec_bytes", "ens_set_profiling", "ens_debug_one_stream", "ens_debug_rows", "ens_debug_stats", "ens_profile_get", "ens_last_ms", "ens_set_combination", "ens_debug_fake_predictor",
            "ens_planner_fit_mem", "ens_planner_wfd", "ens_planner_neighbors", "ens_planner_greedy",
-           "ens_planner_bbs", "ens_partition", "ens_hand_out", "ens_strerror", "ens_version")
+           "ens_planner_bbs", "ens_predict_top", "ens_predict_routed", "ens_route", "ens_route_backward", "ens_combine_routed",
+           "ens_combine_routed_backward", "ens_top", "ens_top_workspace", "ens_distill", "ens_distill_workspace", "ens_distill_backward", "ens_partition", "ens_hand_out", "ens_strerror", "ens_version")
 
 _lib = None
 
@@ -130,6 +135,20 @@ def lib():
         L.ens_planner_bbs.argtypes = [P(EnsPlanProblem), BENCH_SINGLE_FN, vp, P(i32), P(i32)]
         L.ens_partition.argtypes = [i64, i32, i32, P(i64), P(i64), i32, P(i32)]
         L.ens_hand_out.argtypes = [i64, i32, P(i32), i32, dbl, dbl, P(i32), i32, P(i32)]
+        L.ens_predict_top.argtypes = [vp, vp, i64, i32, vp, vp]
+        L.ens_predict_routed.argtypes = [vp, vp, i64, i32, vp, vp, vp]
+        f32 = ctypes.c_float
+        L.ens_route.argtypes = [vp, i32, i64, i64, i32, P(EnsRouteOpts), vp, vp, vp, vp, vp]
+        L.ens_route_backward.argtypes = [vp, i32, i64, i64, i32, P(EnsRouteOpts), vp, vp, vp, i64, vp]
+        L.ens_combine_routed.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, i32, vp, vp, vp]
+        L.ens_combine_routed_backward.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, i32, vp, vp, vp, vp, i64, vp]
+        L.ens_top.argtypes = [vp, i32, i64, i64, i32, i32, i32, f32, vp, vp, vp, i64, vp]
+        L.ens_top_workspace.argtypes = [i64, i32, i32, i32]
+        L.ens_top_workspace.restype = i64
+        L.ens_distill.argtypes = [vp, i32, i64, i64, i32, vp, vp, i32, f32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.ens_distill_workspace.argtypes = [i64, i32, i32, i32]
+        L.ens_distill_workspace.restype = i64
+        L.ens_distill_backward.argtypes = [vp, i32, i64, i64, i32, vp, vp, i32, f32, i32, vp, vp, vp, i64, vp]
         L.ens_strerror.argtypes = [ctypes.c_int]
         L.ens_strerror.restype = ctypes.c_char_p
         L.ens_version.restype = ctypes.c_char_p
@@ -200,6 +219,22 @@ def _sync_producer(tensor):
     device tensor must have landed before the library reads it."""
     import torch
     torch.cuda.current_stream(tensor.device).synchronize()
+
+
+def _need(true, what):
+    if not true:
+        raise ValueError(what)
+
+
+def _whole(buf):
+    return bool(buf.flags["C_CONTIGUOUS"]) if isinstance(buf, np.ndarray) else buf.is_contiguous()
+
+
+def _empty(on_device, beside, shape, kind):
+    if not on_device:
+        return np.empty(shape, dtype=kind)
+    import torch
+    return torch.empty(shape, dtype=getattr(torch, kind), device=beside.device)
 
 
 def make_alloc(matrix):
@@ -306,9 +341,54 @@ class Ensemble:
         _check(lib().ens_predict_static(self._h, _ptr(images), n, _ptr(out)), "ens_predict_static")
         return out
 
-    def ens_member_logits(self, member, n):
-        out = np.empty((n, self.classes), dtype=np.float32)
-        _check(lib().ens_member_logits(self._h, member, n, out.ctypes.data), "ens_member_logits")
+    def ens_predict_top(self, images, k, out=None):
+        """The k most probable classes of every image: (index n x k int32, probability n x k fp32), where ens_predict
+        would put its probabilities.  out: such a pair to write to."""
+        n, images, dev_in = self._request(images)
+        if out is None:
+            out = _empty(dev_in, images, (n, k), "int32"), _empty(dev_in, images, (n, k), "float32")
+        for o, kind in zip(out, ("int32", "float32")):
+            _need(tuple(o.shape) == (n, k) and str(o.dtype).endswith(kind) and _whole(o), "out: two contiguous n x k buffers, int32 and float32")
+        _need(_is_device(out[0]) == _is_device(out[1]), "out: both on the device or both on the host")
+        self._set_io(dev_in, _is_device(out[0]))
+        if dev_in:
+            _sync_producer(images)
+        _check(lib().ens_predict_top(self._h, _ptr(images), n, k, _ptr(out[0]), _ptr(out[1])), "ens_predict_top")
+        return out
+
+    def ens_predict_routed(self, images, chosen, weights, out=None):
+        """ens_predict with each image's own combination: chosen (n x k int32, members) and weights (n x k fp32), on the device if the
+        images are."""
+        n, images, dev_in = self._request(images)
+        _need(tuple(chosen.shape) == tuple(weights.shape) and chosen.ndim == 2 and chosen.shape[0] == n, "chosen and weights are n x k")
+        for o, kind in ((chosen, "int32"), (weights, "float32")):
+            _need(str(o.dtype).endswith(kind) and _whole(o) and _is_device(o) == dev_in, "chosen: int32, weights: float32, contiguous, beside the images")
+        if out is None:
+            out = _empty(dev_in, images, (n, self.classes), "float32")
+        _need(tuple(out.shape) == (n, self.classes) and str(out.dtype).endswith("float32") and _whole(out), "out: contiguous n x classes float32")
+        self._set_io(dev_in, _is_device(out))
+        if dev_in:
+            _sync_producer(images)
+        _check(lib().ens_predict_routed(self._h, _ptr(images), n, int(chosen.shape[1]), _ptr(chosen), _ptr(weights), _ptr(out)), "ens_predict_routed")
+        return out
+
+    def _request(self, images):
+        n = int(images.shape[0])
+        _need(tuple(images.shape[1:]) == (self.base_hw[0], self.base_hw[1], 3), "images: n x %d x %d x 3" % self.base_hw)
+        if isinstance(images, np.ndarray):
+            images = np.ascontiguousarray(images, dtype=np.float32)
+        else:
+            _need(images.is_contiguous() and str(images.dtype) == "torch.float32", "images: contiguous float32")
+        return n, images, _is_device(images)
+
+    def ens_member_logits(self, member, n, out=None):
+        """Host array, or written to `out` (n x classes float32, host or device)."""
+        if out is None:
+            out = np.empty((n, self.classes), dtype=np.float32)
+        _need(tuple(out.shape) == (n, self.classes) and str(out.dtype).endswith("float32") and _whole(out), "out: contiguous n x classes float32")
+        if _is_device(out):
+            _sync_producer(out)                                  # what is still to be read or written there
+        _check(lib().ens_member_logits(self._h, member, n, _ptr(out)), "ens_member_logits")
         return out
 
     def ens_debug_tensor(self, member, tensor, shape_hwc, n_images):
@@ -366,6 +446,188 @@ class Ensemble:
 
     def ens_last_ms(self):
         return lib().ens_last_ms(self._h)
+
+
+# ---- operators on device tensors -----------------------------------------------------------------
+# Kernels go to torch's current stream of the tensors' device; nothing is waited for.  Rows may be strided, the elements of a row may not.
+# They record nothing for autograd: the backward passes are calls of their own.
+
+_SCORE = {"softmax": 0, "sigmoid": 1}
+_FORM = {"value": 0, "log": 1, "log_softmax": 2}
+
+
+def _row_type(t):
+    import torch
+    code = {torch.float32: ENS_FP32, torch.bfloat16: ENS_BF16, torch.float16: ENS_FP16}.get(t.dtype)
+    _need(code is not None, "rows are float32, bfloat16 or float16")
+    return code
+
+
+def _rows(t, what, dims=2):
+    """Distance between the rows of a device tensor."""
+    _need(t.is_cuda and t.dim() == dims, "%s: a device tensor of %d dimensions" % (what, dims))
+    n, length = t.shape[-2], t.shape[-1]
+    _need(length <= 1 or t.stride(-1) == 1, "%s: the elements of a row stand side by side" % what)
+    return t.stride(-2) if n > 1 else max(length, 1)
+
+
+def _plain(t, beside, shape, kind, what):
+    """Address of a contiguous device tensor of that shape and type on the device of `beside`, None for none."""
+    if t is None:
+        return None
+    _need(t.device == beside.device and tuple(t.shape) == tuple(shape) and str(t.dtype) == "torch." + kind and t.is_contiguous(),
+          "%s: contiguous %s of shape %s on %s" % (what, kind, tuple(shape), beside.device))
+    return t.data_ptr()
+
+
+def _issue(beside, name, *args):
+    """A call on the current stream of a tensor's device."""
+    import torch
+    call, where = getattr(lib(), name), beside.device
+    if where.index == torch.cuda.current_device():
+        _check(call(*args, torch.cuda.current_stream(where).cuda_stream), name)
+    else:
+        with torch.cuda.device(where):
+            _check(call(*args, torch.cuda.current_stream(where).cuda_stream), name)
+
+
+def _scratch(bytes_, beside, where):
+    """(tensor, address, size) of a call's workspace."""
+    import torch
+    if bytes_ < 0:
+        _check(int(bytes_), where)
+    if bytes_ == 0:
+        return None, None, 0
+    t = torch.empty(bytes_, dtype=torch.uint8, device=beside.device)
+    return t, t.data_ptr(), bytes_
+
+
+def _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale):
+    _need(score in _SCORE, "score: softmax or sigmoid")
+    return EnsRouteOpts(k, _SCORE[score], groups, groups_kept or groups, group_best, int(bool(renormalise)), scale)
+
+
+def ens_route(gates, k, score="softmax", bias=None, groups=1, groups_kept=None, group_best=2, renormalise=True, scale=1.0, load=None):
+    """The k members that a gate's values (n x members) choose for each row, and their weights: (int32, float32), n x k.
+    load: int32 for each member, to which the rows that chose it are added."""
+    import torch
+    ld, (n, members) = _rows(gates, "gates"), gates.shape
+    opts = _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale)
+    _need(k > 0, "k is positive")
+    chosen = torch.empty((n, k), dtype=torch.int32, device=gates.device)
+    weights = torch.empty((n, k), dtype=torch.float32, device=gates.device)
+    _issue(gates, "ens_route", gates.data_ptr(), _row_type(gates), ld, n, members, ctypes.byref(opts), _plain(bias, gates, (members,), "float32", "bias"),
+           chosen.data_ptr(), weights.data_ptr(), _plain(load, gates, (members,), "int32", "load"))
+    return chosen, weights
+
+
+def ens_route_backward(gates, chosen, d_weights, score="softmax", renormalise=True, scale=1.0):
+    """Gradient of the gate's values, in their type."""
+    import torch
+    ld, (n, members), k = _rows(gates, "gates"), gates.shape, chosen.shape[-1]
+    opts = _route_opts(k, score, 1, 1, 2, renormalise, scale)
+    d_gates = torch.empty((n, members), dtype=gates.dtype, device=gates.device)
+    _issue(gates, "ens_route_backward", gates.data_ptr(), _row_type(gates), ld, n, members, ctypes.byref(opts),
+           _plain(chosen, gates, (n, k), "int32", "chosen"), _plain(d_weights, gates, (n, k), "float32", "d_weights"), d_gates.data_ptr(), members)
+    return d_gates
+
+
+def _member_rows(logits):
+    """(addresses, one of the tensors, distance between rows, members, n, classes) of members' logits: a tensor members x n x classes, or a tensor for each."""
+    if hasattr(logits, "data_ptr"):
+        ld, (members, n, classes) = _rows(logits, "logits", 3), logits.shape
+        first, step = logits.data_ptr(), logits.stride(0) * logits.element_size()
+        return (ctypes.c_void_p * members)(*[first + m * step for m in range(members)]), logits, ld, members, n, classes
+    _need(len(logits) > 0, "a member at least")
+    one = logits[0]
+    ld, (n, classes) = _rows(one, "logits"), one.shape
+    for z in logits:
+        _need(_rows(z, "logits") == ld and z.shape == one.shape and z.dtype == one.dtype and z.device == one.device, "logits of members have one shape, type and device")
+    return (ctypes.c_void_p * len(logits))(*[z.data_ptr() for z in logits]), one, ld, len(logits), n, classes
+
+
+def ens_combine_routed(logits, chosen, weights):
+    """Each row's own combination of the members' softmax outputs.  logits: members x n x classes, or a list of n x classes;
+    chosen, weights: n x k, as ens_route gives them.  Returns the probabilities (n x classes float32) and the state that the backward pass takes."""
+    import torch
+    ptrs, one, ld, members, n, classes = _member_rows(logits)
+    k = chosen.shape[-1]
+    probs = torch.empty((n, classes), dtype=torch.float32, device=one.device)
+    state = torch.empty((n, k, 2), dtype=torch.float32, device=one.device)
+    _issue(one, "ens_combine_routed", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, one, (n, k), "int32", "chosen"),
+           _plain(weights, one, (n, k), "float32", "weights"), k, probs.data_ptr(), state.data_ptr())
+    return probs, state
+
+
+def ens_combine_routed_backward(logits, chosen, weights, state, d_probs, learn=True):
+    """Gradients of the weights (n x k) and of the members' logits, in their type and as they came (a tensor or a list).  learn: whether
+    the members learn, or for a list one truth value each; None stands in the place of a gradient that is not wanted."""
+    import torch
+    ptrs, one, ld, members, n, classes = _member_rows(logits)
+    k = chosen.shape[-1]
+    d_weights = torch.empty((n, k), dtype=torch.float32, device=one.device)
+    if hasattr(logits, "data_ptr"):
+        d_logits = torch.empty((members, n, classes), dtype=one.dtype, device=one.device) if learn else None
+        outs = [d_logits[m] for m in range(members)] if learn else None
+    else:
+        which = [bool(learn)] * members if isinstance(learn, bool) else list(learn)
+        _need(len(which) == members, "learn: a truth value for each member")
+        outs = d_logits = [torch.empty((n, classes), dtype=one.dtype, device=one.device) if w else None for w in which]
+    d_ptrs = (ctypes.c_void_p * members)(*[None if o is None else o.data_ptr() for o in outs]) if outs is not None else None
+    _issue(one, "ens_combine_routed_backward", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, one, (n, k), "int32", "chosen"),
+           _plain(weights, one, (n, k), "float32", "weights"), k, _plain(state, one, (n, k, 2), "float32", "state"),
+           _plain(d_probs, one, (n, classes), "float32", "d_probs"), d_weights.data_ptr(), d_ptrs, classes)
+    return d_weights, d_logits
+
+
+def ens_top(values, k, form="value", temperature=1.0):
+    """The k largest values of each row, largest first, the lowest class first among equal ones: (class int32, float32), n x k.  form: "value",
+    "log", or "log_softmax" (of the row at `temperature`)."""
+    import torch
+    ld, (n, classes) = _rows(values, "values"), values.shape
+    _need(form in _FORM, "form: value, log or log_softmax")
+    _need(k > 0, "k is positive")
+    dtype = _row_type(values)
+    keep, work, size = _scratch(lib().ens_top_workspace(n, classes, k, dtype), values, "ens_top")
+    index = torch.empty((n, k), dtype=torch.int32, device=values.device)
+    value = torch.empty((n, k), dtype=torch.float32, device=values.device)
+    _issue(values, "ens_top", values.data_ptr(), dtype, ld, n, classes, k, _FORM[form], temperature, index.data_ptr(), value.data_ptr(), work, size)
+    return index, value
+
+
+def _gradient_rows(logits, out):
+    import torch
+    if out is None or out is True:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _need(out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device, "the gradient has the logits' shape, type and device")
+    return out, _rows(out, "the gradient")
+
+
+def ens_distill(logits, index, log_probs, temperature=1.0, tail=False, row_weights=None, gradient=False):
+    """Loss of each row of a student's logits (n x classes) against the classes that a teacher kept (index int32, log_probs float32,
+    n x k: ens_top's, with -1 for an entry that is not there): (loss, state).  gradient: True, or a tensor to write to, which may be the
+    logits; then (loss, state, gradient of the sum of row_weights times loss)."""
+    import torch
+    ld, (n, classes), k = _rows(logits, "logits"), logits.shape, index.shape[-1]
+    dtype = _row_type(logits)
+    d, ld_d = (None, 0) if gradient is False or gradient is None else _gradient_rows(logits, gradient)
+    keep, work, size = _scratch(lib().ens_distill_workspace(n, classes, k, dtype), logits, "ens_distill")
+    loss = torch.empty((n,), dtype=torch.float32, device=logits.device)
+    state = torch.empty((n, 3), dtype=torch.float32, device=logits.device)
+    _issue(logits, "ens_distill", logits.data_ptr(), dtype, ld, n, classes, _plain(index, logits, (n, k), "int32", "index"),
+           _plain(log_probs, logits, (n, k), "float32", "log_probs"), k, temperature, int(bool(tail)), _plain(row_weights, logits, (n,), "float32", "row_weights"),
+           loss.data_ptr(), state.data_ptr(), None if d is None else d.data_ptr(), ld_d, work, size)
+    return (loss, state) if d is None else (loss, state, d)
+
+
+def ens_distill_backward(logits, index, log_probs, state, d_loss=None, temperature=1.0, tail=False, out=None):
+    """Gradient of the logits from that of the losses (None: ones), in their type.  out: a tensor to write to, which may be the logits."""
+    ld, (n, classes), k = _rows(logits, "logits"), logits.shape, index.shape[-1]
+    d, ld_d = _gradient_rows(logits, out)
+    _issue(logits, "ens_distill_backward", logits.data_ptr(), _row_type(logits), ld, n, classes, _plain(index, logits, (n, k), "int32", "index"),
+           _plain(log_probs, logits, (n, k), "float32", "log_probs"), k, temperature, int(bool(tail)), _plain(state, logits, (n, 3), "float32", "state"),
+           _plain(d_loss, logits, (n,), "float32", "d_loss"), d.data_ptr(), ld_d)
+    return d
 
 
 def ens_spec_bytes(net, batch):

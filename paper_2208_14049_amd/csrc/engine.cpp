@@ -14,6 +14,7 @@
 #include <cstring>
 
 #include "chain.h"
+#include "operators.h"
 #include "planner.h"
 #include "resident.h"
 #include "seedgen.h"
@@ -1950,6 +1951,22 @@ static int time_installed(ens_handle* h, int64_t n, int repeats, uint64_t mask, 
     return ENS_OK;
 }
 
+// A request whose probabilities go to d_probs on the device whatever ens_set_io says, and the work that `behind` issues on the handle's own stream
+// after it, waited for whether all of it could be issued or not.
+template <class F>
+static int predict_and(ens_handle* h, const float* images, int64_t n, float* d_probs, F&& behind) {
+    const auto t0 = std::chrono::steady_clock::now();
+    const bool on_device = h->probs_on_device;
+    h->probs_on_device = true;
+    int rc = ens_predict(h, images, n, d_probs);
+    h->probs_on_device = on_device;
+    if (rc != ENS_OK) return rc;
+    rc = behind();
+    HIP_TRY(hipStreamSynchronize(h->main_stream));
+    h->last_ms = std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - t0).count();
+    return rc;
+}
+
 }  // namespace ens
 
 // ------------------------------------------------------------------------------------ C API
@@ -2123,6 +2140,68 @@ int ens_predict_static(ens_handle* h, const float* d_images, int64_t n, float* d
     return ENS_OK;
 }
 
+int ens_predict_top(ens_handle* h, const float* images, int64_t n, int32_t k, int32_t* index_out, float* prob_out) {
+    if (!h || n < 0 || k < 1 || k > h->classes || (n > 0 && (!images || !index_out || !prob_out))) return ENS_E_INVALID;
+    if (k > TOP_MAX_K) return ENS_E_UNSUPPORTED;
+    if (n == 0) return ENS_OK;
+    if (!h->have_alloc) {
+        const int rc = default_alloc(h);
+        if (rc != ENS_OK) return rc;
+    }
+    // probabilities, the kept ones and their classes, the operator's workspace
+    const size_t probs = ((size_t)n * h->classes + 1) / 2 * 2, kept = ((size_t)n * k + 1) / 2 * 2;
+    const int64_t workspace = top_workspace(n, h->classes, k, ENS_FP32);
+    const int rc = with_room(h, [&] { return grow(&h->d_probs, &h->d_probs_cap, probs + 2 * kept + (size_t)(workspace + 3) / 4); });
+    if (rc != ENS_OK) return rc;
+    return predict_and(h, images, n, h->d_probs, [&]() -> int {
+        TopArgs a{};
+        a.values = h->d_probs; a.ld = h->classes; a.n = n; a.dtype = ENS_FP32; a.classes = h->classes; a.k = k;
+        a.inv_temperature = 1.f;
+        a.value = h->probs_on_device ? prob_out : h->d_probs + probs;
+        a.index = h->probs_on_device ? index_out : (int32_t*)(h->d_probs + probs + kept);
+        a.workspace = h->d_probs + probs + 2 * kept;
+        HIP_TRY(launch_top(a, h->main_stream));
+        if (h->probs_on_device) return ENS_OK;
+        HIP_TRY(hipMemcpyAsync(prob_out, a.value, (size_t)n * k * sizeof(float), hipMemcpyDeviceToHost, h->main_stream));
+        HIP_TRY(hipMemcpyAsync(index_out, a.index, (size_t)n * k * sizeof(int32_t), hipMemcpyDeviceToHost, h->main_stream));
+        return ENS_OK;
+    });
+}
+
+int ens_predict_routed(ens_handle* h, const float* images, int64_t n, int32_t k, const int32_t* chosen, const float* weights, float* probs_out) {
+    if (!h || n < 0 || k < 1 || (n > 0 && (!images || !chosen || !weights || !probs_out))) return ENS_E_INVALID;
+    if (k > ROUTED_MAX_K) return ENS_E_UNSUPPORTED;
+    if (n == 0) return ENS_OK;
+    if (!h->have_alloc) {
+        const int rc = default_alloc(h);
+        if (rc != ENS_OK) return rc;
+    }
+    const size_t probs = (size_t)n * h->classes, choices = (size_t)n * k;
+    const size_t here = h->probs_on_device ? 0 : probs, want = here + (h->images_on_device ? 0 : 2 * choices);
+    const int rc = want ? with_room(h, [&] { return grow(&h->d_probs, &h->d_probs_cap, want); }) : ENS_OK;
+    if (rc != ENS_OK) return rc;
+    float* const d_out = h->probs_on_device ? probs_out : h->d_probs;
+    // the request ends in the handle's own rule, whose place the routed one takes
+    return predict_and(h, images, n, d_out, [&]() -> int {
+        RoutedArgs a{};
+        for (size_t m = 0; m < h->members.size(); m++) a.logits[m] = h->d_logits[m];
+        a.ld = h->classes; a.n = n; a.dtype = ENS_FP32; a.members = (int)h->members.size(); a.classes = h->classes; a.k = k;
+        a.chosen = chosen; a.weights = weights;
+        if (!h->images_on_device) {
+            float* const d_weights = h->d_probs + here;
+            int32_t* const d_chosen = (int32_t*)(d_weights + choices);
+            HIP_TRY(hipMemcpyAsync(d_weights, weights, choices * sizeof(float), hipMemcpyHostToDevice, h->main_stream));
+            HIP_TRY(hipMemcpyAsync(d_chosen, chosen, choices * sizeof(int32_t), hipMemcpyHostToDevice, h->main_stream));
+            a.chosen = d_chosen; a.weights = d_weights;
+        }
+        a.probs = d_out;
+        HIP_TRY(launch_combine_routed(a, h->main_stream));
+        if (!h->probs_on_device)
+            HIP_TRY(hipMemcpyAsync(probs_out, d_out, probs * sizeof(float), hipMemcpyDeviceToHost, h->main_stream));
+        return ENS_OK;
+    });
+}
+
 int ens_static_scratch_bytes(void) { return (int)STATIC_SCRATCH_BYTES; }
 
 int ens_bench(ens_handle* h, const ens_alloc* a, int32_t segment_size, int64_t n_calib, int32_t repeats,
@@ -2265,8 +2344,8 @@ int ens_plan(ens_handle* h, uint64_t mem_budget_bytes, const ens_plan_opts* opts
 int ens_member_logits(ens_handle* h, int32_t member, int64_t n, float* logits_out) {
     if (!h || member < 0 || member >= (int)h->members.size() || !logits_out) return ENS_E_INVALID;
     if (n <= 0 || n > h->last_n || (size_t)n > h->d_logits_rows) return ENS_E_INVALID;
-    HIP_TRY(hipMemcpy(logits_out, h->d_logits[member], (size_t)n * h->members[member].classes * sizeof(float),
-                      hipMemcpyDeviceToHost));
+    HIP_TRY(hipMemcpy(logits_out, h->d_logits[member], (size_t)n * h->members[member].classes * sizeof(float), hipMemcpyDefault));
+    HIP_TRY(hipStreamSynchronize(nullptr));                      // a copy within the device is not waited for by itself
     return ENS_OK;
 }
 

@@ -1,0 +1,162 @@
+// Rows of logits, probabilities or scores in fp32, bf16 or fp16: how a workgroup or a wavefront walks one in 16-byte pieces wherever it
+// begins, and the reductions over it.  All arithmetic is fp32.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ens {
+
+constexpr float LOWEST = -3.402823466e38f;   // running maxima start here: minus infinity less this is minus infinity, not NaN
+constexpr float NONE = -__builtin_inff();
+constexpr float LOG2E = 1.44269504088896341f;
+
+template <class T> constexpr int PIECE = 16 / (int)sizeof(T);   // elements of 16 bytes
+
+__device__ __forceinline__ float up(float v) { return v; }
+__device__ __forceinline__ float up(__bf16 v) { return (float)v; }
+__device__ __forceinline__ float up(_Float16 v) { return (float)v; }
+
+__device__ __forceinline__ void unpack(const uint4& u, float (&f)[4], const float*) {
+    f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ void unpack(const uint4& u, float (&f)[8], const __bf16*) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        f[2 * e] = __uint_as_float(w[e] << 16);
+        f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint4& u, float (&f)[8], const _Float16*) {
+    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+    const half8 h = __builtin_bit_cast(half8, u);
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = (float)h[e];
+}
+// To the row's type, to nearest even.
+__device__ __forceinline__ uint4 pack(const float (&f)[4], const float*) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[8], const __bf16*) {
+    typedef float float8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+    const float8 v = {f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
+    return __builtin_bit_cast(uint4, __builtin_convertvector(v, bf8));
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[8], const _Float16*) {
+    typedef float float8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+    const float8 v = {f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
+    return __builtin_bit_cast(uint4, __builtin_convertvector(v, half8));
+}
+
+// e^d for d <= 0.  The argument is a difference to a maximum, so that its product with log2 e is off by 2^-24 of itself, and the
+// hardware's power of two by one unit more.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
+
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+// A running maximum and the sum of e^((x - m) c) that goes with it.
+struct MaxSum { float m, s; };
+__device__ __forceinline__ MaxSum join(const MaxSum a, const MaxSum b, const float c) {
+    const float m = fmaxf(a.m, b.m);
+    return MaxSum{m, a.s * exp_of((a.m - m) * c) + b.s * exp_of((b.m - m) * c)};
+}
+
+// A row of `len` elements from `p` on, in any alignment to its elements: the elements in front of the first 16-byte boundary and those
+// behind the last whole piece are taken one to a thread, the pieces between them in turn by all.
+template <class T, int THREADS>
+struct Row {
+    const T* p;
+    int len, head, pieces;
+    __device__ __forceinline__ Row(const T* row, int n) : p(row), len(n) {
+        head = (int)((16u - ((unsigned)(uintptr_t)row & 15u)) & 15u) / (int)sizeof(T);
+        if (head > n) head = n;
+        pieces = (n - head) / PIECE<T>;
+    }
+    __device__ __forceinline__ const uint4* body() const { return (const uint4*)(p + head); }
+    // The single element of this thread, or -1.
+    __device__ __forceinline__ int single(int tid) const {
+        if (tid < head) return tid;
+        const int c = head + pieces * PIECE<T> + tid - PIECE<T>;
+        return tid >= PIECE<T> && c < len ? c : -1;
+    }
+    // f(value, class) over this thread's share
+    template <class F>
+    __device__ __forceinline__ void each(int tid, F f) const {
+        const int one = single(tid);
+        if (one >= 0) f(up(p[one]), one);
+        for (int i = tid; i < pieces; i += THREADS) {
+            float v[PIECE<T>];
+            unpack(body()[i], v, p);
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) f(v[e], head + i * PIECE<T> + e);
+        }
+    }
+    // The same, f(value, class) -> value to be stored at dst[class]; in 16-byte pieces where dst has the row's alignment.  dst may be p.
+    template <class F>
+    __device__ __forceinline__ void map(int tid, T* dst, F f) const {
+        const int one = single(tid);
+        if (one >= 0) dst[one] = (T)f(up(p[one]), one);
+        const bool alike = (((uintptr_t)dst - (uintptr_t)p) & 15u) == 0;
+        for (int i = tid; i < pieces; i += THREADS) {
+            float v[PIECE<T>];
+            unpack(body()[i], v, p);
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) v[e] = f(v[e], head + i * PIECE<T> + e);
+            if (alike) *(uint4*)(dst + head + i * PIECE<T>) = pack(v, p);
+            else
+#pragma unroll
+                for (int e = 0; e < PIECE<T>; e++) dst[head + i * PIECE<T> + e] = (T)v[e];
+        }
+    }
+};
+
+// Over a workgroup; `box`: a float for each of its wavefronts.  Every thread gets the result, added or compared in the same order.
+template <int THREADS>
+__device__ __forceinline__ float group_max(float v, float* box) {
+    v = lanes_max(v);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = box[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; w++) v = fmaxf(v, box[w]);
+    }
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ float group_sum(float v, float* box) {
+    v = lanes_sum(v);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = box[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; w++) v += box[w];
+    }
+    return v;
+}
+
+// Calls f with a value of the type that `dtype` (ENS_FP32, ENS_BF16, ENS_FP16) names.
+template <class F>
+static inline hipError_t by_type(int dtype, F f) {
+    switch (dtype) {
+        case 0: return f((float)0);
+        case 1: return f((__bf16)0.f);
+        case 2: return f((_Float16)0.f);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace ens
