@@ -456,106 +456,123 @@ _SCORE = {"softmax": 0, "sigmoid": 1}
 _FORM = {"value": 0, "log": 1, "log_softmax": 2}
 
 
+_row_types = {}
+
+
 def _row_type(t):
-    import torch
-    code = {torch.float32: ENS_FP32, torch.bfloat16: ENS_BF16, torch.float16: ENS_FP16}.get(t.dtype)
-    _need(code is not None, "rows are float32, bfloat16 or float16")
+    """ENS_* of a row tensor's type."""
+    if not _row_types:
+        import torch
+        _row_types.update({torch.float32: ENS_FP32, torch.bfloat16: ENS_BF16, torch.float16: ENS_FP16})
+    code = _row_types.get(t.dtype)
+    if code is None:
+        raise ValueError("rows are float32, bfloat16 or float16")
     return code
 
 
 def _rows(t, what, dims=2):
-    """Distance between the rows of a device tensor."""
-    _need(t.is_cuda and t.dim() == dims, "%s: a device tensor of %d dimensions" % (what, dims))
-    n, length = t.shape[-2], t.shape[-1]
-    _need(length <= 1 or t.stride(-1) == 1, "%s: the elements of a row stand side by side" % what)
-    return t.stride(-2) if n > 1 else max(length, 1)
+    """Shape of a device tensor of rows, and the distance between them."""
+    shape = t.shape
+    if not t.is_cuda or len(shape) != dims:
+        raise ValueError("%s: a device tensor of %d dimensions" % (what, dims))
+    stride = t.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError("%s: the elements of a row stand side by side" % what)
+    return shape, stride[-2] if shape[-2] > 1 else max(shape[-1], 1)
 
 
-def _plain(t, beside, shape, kind, what):
-    """Address of a contiguous device tensor of that shape and type on the device of `beside`, None for none."""
+def _plain(t, device, shape, dtype, what):
+    """Address of a contiguous tensor of that shape and type on that device, None for none."""
     if t is None:
         return None
-    _need(t.device == beside.device and tuple(t.shape) == tuple(shape) and str(t.dtype) == "torch." + kind and t.is_contiguous(),
-          "%s: contiguous %s of shape %s on %s" % (what, kind, tuple(shape), beside.device))
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: contiguous %s of shape %s on %s" % (what, dtype, tuple(shape), device))
     return t.data_ptr()
 
 
-def _issue(beside, name, *args):
-    """A call on the current stream of a tensor's device."""
-    import torch
-    call, where = getattr(lib(), name), beside.device
-    if where.index == torch.cuda.current_device():
-        _check(call(*args, torch.cuda.current_stream(where).cuda_stream), name)
+def _issue(device, name, *args):
+    """A call on the current stream of a device."""
+    from torch import cuda
+    call = getattr(lib(), name)
+    if device.index == cuda.current_device():
+        rc = call(*args, cuda.current_stream(device).cuda_stream)
     else:
-        with torch.cuda.device(where):
-            _check(call(*args, torch.cuda.current_stream(where).cuda_stream), name)
+        with cuda.device(device):
+            rc = call(*args, cuda.current_stream(device).cuda_stream)
+    if rc != ENS_OK:
+        raise EnsError(rc, name)
 
 
-def _scratch(bytes_, beside, where):
-    """(tensor, address, size) of a call's workspace."""
+def _scratch(size, device, where):
+    """A call's workspace (None where it needs none) and its address."""
+    if size == 0:
+        return None, None
+    if size < 0:
+        raise EnsError(int(size), where)
     import torch
-    if bytes_ < 0:
-        _check(int(bytes_), where)
-    if bytes_ == 0:
-        return None, None, 0
-    t = torch.empty(bytes_, dtype=torch.uint8, device=beside.device)
-    return t, t.data_ptr(), bytes_
+    t = torch.empty(size, dtype=torch.uint8, device=device)
+    return t, t.data_ptr()
 
 
 def _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale):
-    _need(score in _SCORE, "score: softmax or sigmoid")
-    return EnsRouteOpts(k, _SCORE[score], groups, groups_kept or groups, group_best, int(bool(renormalise)), scale)
+    if score not in _SCORE:
+        raise ValueError("score: softmax or sigmoid")
+    if k < 1:
+        raise ValueError("k is positive")
+    return EnsRouteOpts(k, _SCORE[score], groups, groups_kept or groups, group_best, 1 if renormalise else 0, scale)
 
 
 def ens_route(gates, k, score="softmax", bias=None, groups=1, groups_kept=None, group_best=2, renormalise=True, scale=1.0, load=None):
     """The k members that a gate's values (n x members) choose for each row, and their weights: (int32, float32), n x k.
     load: int32 for each member, to which the rows that chose it are added."""
     import torch
-    ld, (n, members) = _rows(gates, "gates"), gates.shape
-    opts = _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale)
-    _need(k > 0, "k is positive")
-    chosen = torch.empty((n, k), dtype=torch.int32, device=gates.device)
-    weights = torch.empty((n, k), dtype=torch.float32, device=gates.device)
-    _issue(gates, "ens_route", gates.data_ptr(), _row_type(gates), ld, n, members, ctypes.byref(opts), _plain(bias, gates, (members,), "float32", "bias"),
-           chosen.data_ptr(), weights.data_ptr(), _plain(load, gates, (members,), "int32", "load"))
+    (n, members), ld = _rows(gates, "gates")
+    opts, where = _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale), gates.device
+    chosen = torch.empty((n, k), dtype=torch.int32, device=where)
+    weights = torch.empty((n, k), dtype=torch.float32, device=where)
+    _issue(where, "ens_route", gates.data_ptr(), _row_type(gates), ld, n, members, opts, _plain(bias, where, (members,), torch.float32, "bias"),
+           chosen.data_ptr(), weights.data_ptr(), _plain(load, where, (members,), torch.int32, "load"))
     return chosen, weights
 
 
 def ens_route_backward(gates, chosen, d_weights, score="softmax", renormalise=True, scale=1.0):
     """Gradient of the gate's values, in their type."""
     import torch
-    ld, (n, members), k = _rows(gates, "gates"), gates.shape, chosen.shape[-1]
+    (n, members), ld = _rows(gates, "gates")
+    k, where = chosen.shape[-1], gates.device
     opts = _route_opts(k, score, 1, 1, 2, renormalise, scale)
-    d_gates = torch.empty((n, members), dtype=gates.dtype, device=gates.device)
-    _issue(gates, "ens_route_backward", gates.data_ptr(), _row_type(gates), ld, n, members, ctypes.byref(opts),
-           _plain(chosen, gates, (n, k), "int32", "chosen"), _plain(d_weights, gates, (n, k), "float32", "d_weights"), d_gates.data_ptr(), members)
+    d_gates = torch.empty((n, members), dtype=gates.dtype, device=where)
+    _issue(where, "ens_route_backward", gates.data_ptr(), _row_type(gates), ld, n, members, opts, _plain(chosen, where, (n, k), torch.int32, "chosen"),
+           _plain(d_weights, where, (n, k), torch.float32, "d_weights"), d_gates.data_ptr(), members)
     return d_gates
 
 
 def _member_rows(logits):
-    """(addresses, one of the tensors, distance between rows, members, n, classes) of members' logits: a tensor members x n x classes, or a tensor for each."""
+    """(addresses, one of the tensors, members, n, classes, distance between rows) of members' logits: a tensor members x n x classes, or a tensor for each."""
     if hasattr(logits, "data_ptr"):
-        ld, (members, n, classes) = _rows(logits, "logits", 3), logits.shape
+        (members, n, classes), ld = _rows(logits, "logits", 3)
         first, step = logits.data_ptr(), logits.stride(0) * logits.element_size()
-        return (ctypes.c_void_p * members)(*[first + m * step for m in range(members)]), logits, ld, members, n, classes
-    _need(len(logits) > 0, "a member at least")
+        return (ctypes.c_void_p * members)(*range(first, first + members * step, step) if step else [first] * members), logits, members, n, classes, ld
+    if len(logits) == 0:
+        raise ValueError("a member at least")
     one = logits[0]
-    ld, (n, classes) = _rows(one, "logits"), one.shape
+    (n, classes), ld = shape = _rows(one, "logits")
     for z in logits:
-        _need(_rows(z, "logits") == ld and z.shape == one.shape and z.dtype == one.dtype and z.device == one.device, "logits of members have one shape, type and device")
-    return (ctypes.c_void_p * len(logits))(*[z.data_ptr() for z in logits]), one, ld, len(logits), n, classes
+        if _rows(z, "logits") != shape or z.dtype != one.dtype or z.device != one.device:
+            raise ValueError("logits of members have one shape, row distance, type and device")
+    return (ctypes.c_void_p * len(logits))(*[z.data_ptr() for z in logits]), one, len(logits), n, classes, ld
 
 
 def ens_combine_routed(logits, chosen, weights):
     """Each row's own combination of the members' softmax outputs.  logits: members x n x classes, or a list of n x classes;
     chosen, weights: n x k, as ens_route gives them.  Returns the probabilities (n x classes float32) and the state that the backward pass takes."""
     import torch
-    ptrs, one, ld, members, n, classes = _member_rows(logits)
-    k = chosen.shape[-1]
-    probs = torch.empty((n, classes), dtype=torch.float32, device=one.device)
-    state = torch.empty((n, k, 2), dtype=torch.float32, device=one.device)
-    _issue(one, "ens_combine_routed", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, one, (n, k), "int32", "chosen"),
-           _plain(weights, one, (n, k), "float32", "weights"), k, probs.data_ptr(), state.data_ptr())
+    ptrs, one, members, n, classes, ld = _member_rows(logits)
+    k, where = chosen.shape[-1], one.device
+    probs = torch.empty((n, classes), dtype=torch.float32, device=where)
+    state = torch.empty((n, k, 2), dtype=torch.float32, device=where)
+    _issue(where, "ens_combine_routed", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, where, (n, k), torch.int32, "chosen"),
+           _plain(weights, where, (n, k), torch.float32, "weights"), k, probs.data_ptr(), state.data_ptr())
     return probs, state
 
 
@@ -563,20 +580,24 @@ def ens_combine_routed_backward(logits, chosen, weights, state, d_probs, learn=T
     """Gradients of the weights (n x k) and of the members' logits, in their type and as they came (a tensor or a list).  learn: whether
     the members learn, or for a list one truth value each; None stands in the place of a gradient that is not wanted."""
     import torch
-    ptrs, one, ld, members, n, classes = _member_rows(logits)
-    k = chosen.shape[-1]
-    d_weights = torch.empty((n, k), dtype=torch.float32, device=one.device)
+    ptrs, one, members, n, classes, ld = _member_rows(logits)
+    k, where = chosen.shape[-1], one.device
+    d_weights = torch.empty((n, k), dtype=torch.float32, device=where)
+    d_logits, d_ptrs = None, None
     if hasattr(logits, "data_ptr"):
-        d_logits = torch.empty((members, n, classes), dtype=one.dtype, device=one.device) if learn else None
-        outs = [d_logits[m] for m in range(members)] if learn else None
+        if learn:
+            d_logits = torch.empty((members, n, classes), dtype=one.dtype, device=where)
+            first, step = d_logits.data_ptr(), n * classes * one.element_size()
+            d_ptrs = (ctypes.c_void_p * members)(*[first + m * step for m in range(members)])
     else:
         which = [bool(learn)] * members if isinstance(learn, bool) else list(learn)
-        _need(len(which) == members, "learn: a truth value for each member")
-        outs = d_logits = [torch.empty((n, classes), dtype=one.dtype, device=one.device) if w else None for w in which]
-    d_ptrs = (ctypes.c_void_p * members)(*[None if o is None else o.data_ptr() for o in outs]) if outs is not None else None
-    _issue(one, "ens_combine_routed_backward", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, one, (n, k), "int32", "chosen"),
-           _plain(weights, one, (n, k), "float32", "weights"), k, _plain(state, one, (n, k, 2), "float32", "state"),
-           _plain(d_probs, one, (n, classes), "float32", "d_probs"), d_weights.data_ptr(), d_ptrs, classes)
+        if len(which) != members:
+            raise ValueError("learn: a truth value for each member")
+        d_logits = [torch.empty((n, classes), dtype=one.dtype, device=where) if w else None for w in which]
+        d_ptrs = (ctypes.c_void_p * members)(*[None if d is None else d.data_ptr() for d in d_logits])
+    _issue(where, "ens_combine_routed_backward", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, where, (n, k), torch.int32, "chosen"),
+           _plain(weights, where, (n, k), torch.float32, "weights"), k, _plain(state, where, (n, k, 2), torch.float32, "state"),
+           _plain(d_probs, where, (n, classes), torch.float32, "d_probs"), d_weights.data_ptr(), d_ptrs, classes)
     return d_weights, d_logits
 
 
@@ -584,23 +605,28 @@ def ens_top(values, k, form="value", temperature=1.0):
     """The k largest values of each row, largest first, the lowest class first among equal ones: (class int32, float32), n x k.  form: "value",
     "log", or "log_softmax" (of the row at `temperature`)."""
     import torch
-    ld, (n, classes) = _rows(values, "values"), values.shape
-    _need(form in _FORM, "form: value, log or log_softmax")
-    _need(k > 0, "k is positive")
-    dtype = _row_type(values)
-    keep, work, size = _scratch(lib().ens_top_workspace(n, classes, k, dtype), values, "ens_top")
-    index = torch.empty((n, k), dtype=torch.int32, device=values.device)
-    value = torch.empty((n, k), dtype=torch.float32, device=values.device)
-    _issue(values, "ens_top", values.data_ptr(), dtype, ld, n, classes, k, _FORM[form], temperature, index.data_ptr(), value.data_ptr(), work, size)
+    (n, classes), ld = _rows(values, "values")
+    if form not in _FORM:
+        raise ValueError("form: value, log or log_softmax")
+    if k < 1:
+        raise ValueError("k is positive")
+    dtype, where = _row_type(values), values.device
+    size = lib().ens_top_workspace(n, classes, k, dtype)
+    keep, work = _scratch(size, where, "ens_top")
+    index = torch.empty((n, k), dtype=torch.int32, device=where)
+    value = torch.empty((n, k), dtype=torch.float32, device=where)
+    _issue(where, "ens_top", values.data_ptr(), dtype, ld, n, classes, k, _FORM[form], temperature, index.data_ptr(), value.data_ptr(), work, size)
     return index, value
 
 
 def _gradient_rows(logits, out):
-    import torch
+    """The tensor that a gradient goes to, and the distance between its rows."""
     if out is None or out is True:
+        import torch
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _need(out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device, "the gradient has the logits' shape, type and device")
-    return out, _rows(out, "the gradient")
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
+        raise ValueError("the gradient has the logits' shape, type and device")
+    return out, _rows(out, "the gradient")[1]
 
 
 def ens_distill(logits, index, log_probs, temperature=1.0, tail=False, row_weights=None, gradient=False):
@@ -608,25 +634,28 @@ def ens_distill(logits, index, log_probs, temperature=1.0, tail=False, row_weigh
     n x k: ens_top's, with -1 for an entry that is not there): (loss, state).  gradient: True, or a tensor to write to, which may be the
     logits; then (loss, state, gradient of the sum of row_weights times loss)."""
     import torch
-    ld, (n, classes), k = _rows(logits, "logits"), logits.shape, index.shape[-1]
-    dtype = _row_type(logits)
+    (n, classes), ld = _rows(logits, "logits")
+    k, dtype, where = index.shape[-1], _row_type(logits), logits.device
     d, ld_d = (None, 0) if gradient is False or gradient is None else _gradient_rows(logits, gradient)
-    keep, work, size = _scratch(lib().ens_distill_workspace(n, classes, k, dtype), logits, "ens_distill")
-    loss = torch.empty((n,), dtype=torch.float32, device=logits.device)
-    state = torch.empty((n, 3), dtype=torch.float32, device=logits.device)
-    _issue(logits, "ens_distill", logits.data_ptr(), dtype, ld, n, classes, _plain(index, logits, (n, k), "int32", "index"),
-           _plain(log_probs, logits, (n, k), "float32", "log_probs"), k, temperature, int(bool(tail)), _plain(row_weights, logits, (n,), "float32", "row_weights"),
-           loss.data_ptr(), state.data_ptr(), None if d is None else d.data_ptr(), ld_d, work, size)
+    size = lib().ens_distill_workspace(n, classes, k, dtype)
+    keep, work = _scratch(size, where, "ens_distill")
+    loss = torch.empty((n,), dtype=torch.float32, device=where)
+    state = torch.empty((n, 3), dtype=torch.float32, device=where)
+    _issue(where, "ens_distill", logits.data_ptr(), dtype, ld, n, classes, _plain(index, where, (n, k), torch.int32, "index"),
+           _plain(log_probs, where, (n, k), torch.float32, "log_probs"), k, temperature, 1 if tail else 0,
+           _plain(row_weights, where, (n,), torch.float32, "row_weights"), loss.data_ptr(), state.data_ptr(), None if d is None else d.data_ptr(), ld_d, work, size)
     return (loss, state) if d is None else (loss, state, d)
 
 
 def ens_distill_backward(logits, index, log_probs, state, d_loss=None, temperature=1.0, tail=False, out=None):
     """Gradient of the logits from that of the losses (None: ones), in their type.  out: a tensor to write to, which may be the logits."""
-    ld, (n, classes), k = _rows(logits, "logits"), logits.shape, index.shape[-1]
+    import torch
+    (n, classes), ld = _rows(logits, "logits")
+    k, where = index.shape[-1], logits.device
     d, ld_d = _gradient_rows(logits, out)
-    _issue(logits, "ens_distill_backward", logits.data_ptr(), _row_type(logits), ld, n, classes, _plain(index, logits, (n, k), "int32", "index"),
-           _plain(log_probs, logits, (n, k), "float32", "log_probs"), k, temperature, int(bool(tail)), _plain(state, logits, (n, 3), "float32", "state"),
-           _plain(d_loss, logits, (n,), "float32", "d_loss"), d.data_ptr(), ld_d)
+    _issue(where, "ens_distill_backward", logits.data_ptr(), _row_type(logits), ld, n, classes, _plain(index, where, (n, k), torch.int32, "index"),
+           _plain(log_probs, where, (n, k), torch.float32, "log_probs"), k, temperature, 1 if tail else 0, _plain(state, where, (n, 3), torch.float32, "state"),
+           _plain(d_loss, where, (n,), torch.float32, "d_loss"), d.data_ptr(), ld_d)
     return d
 
 

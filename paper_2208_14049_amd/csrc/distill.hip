@@ -14,178 +14,406 @@
 
 namespace ens {
 
-constexpr int DISTILL_THREADS = 256;
+constexpr int KEPT_LANES = DISTILL_MAX_K / 64;
 
-// The teacher's record of a row, in LDS.  A wavefront reads it: entry j's class or -1, its q, and of them sum and rest.
+// The teacher's record of a row in LDS, as a wavefront leaves it: class (or -1) and q of k entries, the sum of q, q_0, and the sum of q ln q.
 struct Record {
-    int* index;                  // k
-    float* q;                    // k
-    float* sums;                 // sum of q, q_0, q ln q of all entries and q_0
+    int* index;
+    float* q;
+    float* sums;
 };
 __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, int lane, const Record& r) {
     const int32_t* const index = a.index + row * a.k;
     const float* const log_probs = a.log_probs + row * a.k;
-    float top = NONE;
+    int c[KEPT_LANES];
+    float q[KEPT_LANES], top = NONE, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < KEPT_LANES; i++) {
+        const int j = 64 * i + lane;
+        c[i] = j < a.k ? index[j] : -1;
+        q[i] = j < a.k ? log_probs[j] : NONE;
+        if (c[i] < 0 || c[i] >= a.classes) {
+            c[i] = -1;
+            q[i] = NONE;
+        }
+        top = fmaxf(top, q[i]);
+    }
+    top = a.tail ? 0.f : lanes_max(top);
+#pragma unroll
+    for (int i = 0; i < KEPT_LANES; i++) {
+        q[i] = q[i] == NONE ? 0.f : expf(q[i] - top);
+        sum += q[i];
+    }
     if (!a.tail) {
-        for (int j = lane; j < a.k; j += 64)
-            if (index[j] >= 0 && index[j] < a.classes) top = fmaxf(top, log_probs[j]);
-        top = lanes_max(top);
+        sum = lanes_sum(sum);
+        const float scale = sum == 0.f ? 1.f : 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < KEPT_LANES; i++) q[i] *= scale;
     }
-    float sum = 0.f;
-    for (int j = lane; j < a.k; j += 64) {
-        const int c = index[j];
-        const bool here = c >= 0 && c < a.classes;
-        const float t = here ? log_probs[j] : NONE;
-        const float q = t == NONE ? 0.f : expf(a.tail ? t : t - top);
-        r.index[j] = here ? c : -1;
-        r.q[j] = q;
-        sum += q;
-    }
-    sum = lanes_sum(sum);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const float scale = a.tail || sum == 0.f ? 1.f : 1.f / sum;
     // the first entry of a class takes what the later ones have
-    for (int j0 = 0; j0 < a.k; j0 += 64) {
-        const int j = j0 + lane;
-        float q = 0.f;
-        int c = -1;
-        if (j < a.k) {
-            c = r.index[j];
-            bool first = true;
-            for (int i = 0; i < a.k; i++) {
-                const int other = r.index[i];
-                if (other == c) {
-                    if (i < j) first = false;
-                    q += r.q[i];
-                }
-            }
-            if (!first) c = -2;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (j < a.k) {
-            r.index[j + a.k] = c < 0 ? -1 : c;
-            r.q[j + a.k] = c < 0 ? 0.f : q * scale;
-        }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     float mass = 0.f, entropy = 0.f;
-    for (int j = lane; j < a.k; j += 64) {
-        const float q = r.q[j + a.k];
-        mass += q;
-        if (q != 0.f) entropy += q * logf(q);
+#pragma unroll
+    for (int i = 0; i < KEPT_LANES; i++) {
+        if (64 * i >= a.k) break;
+        const int j = 64 * i + lane;
+        float all = 0.f;
+        bool first = c[i] >= 0;
+#pragma unroll
+        for (int o = 0; o < KEPT_LANES; o++) {
+            const int entries = min(64, a.k - 64 * o);
+            for (int l = 0; l < entries; l++) {
+                const bool same = c[i] == __builtin_amdgcn_readlane(c[o], l);
+                all += same ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q[o]), l)) : 0.f;
+                if (64 * o + l < j) first = first && !same;
+            }
+        }
+        if (!first) all = 0.f;
+        if (j < a.k) {
+            r.index[j] = first ? c[i] : -1;
+            r.q[j] = all;
+        }
+        mass += all;
+        if (all != 0.f) entropy += all * logf(all);
     }
     mass = lanes_sum(mass);
     entropy = lanes_sum(entropy);
-    const float rest = a.tail ? fmaxf(0.f, 1.f - mass) : 0.f;
     if (lane == 0) {
         r.sums[0] = mass;
-        r.sums[1] = rest;
+        r.sums[1] = a.tail ? fmaxf(0.f, 1.f - mass) : 0.f;
         r.sums[2] = entropy;
     }
 }
 
-// LDS: the record twice (as read, and with equal classes joined), three sums, a float for each wavefront; a bit for each class (tail)
-static __host__ __device__ int distill_lds(int k, int classes, bool tail) {
-    return (4 * k + 3 + DISTILL_THREADS / 64) * 4 + (tail ? (classes + 31) / 32 * 4 : 0);
+// A bit for each class, set for those that are kept: bit PIECE + c - head, so that a piece's bits stand together, in a byte or half a byte.
+// Piece `first` + tid, `first` even.
+template <class T>
+__device__ __forceinline__ uint32_t piece_marks(const uint32_t* marks, int first, int tid) {
+    const uint8_t* const bytes = (const uint8_t*)marks;
+    if constexpr (PIECE<T> == 8) return bytes[tid + 1 + first];
+    else return bytes[((tid + 1) >> 1) + (first >> 1)] >> (4 * ((tid + 1) & 1)) & 15u;
+}
+static __host__ __device__ int mark_words(int pieces, int piece) { return ((pieces + 2) * piece + 31) / 32; }
+
+// e of a piece into the sums over kept classes and others
+template <int N>
+__device__ __forceinline__ void add_piece(const float (&e)[N], uint32_t marked, float& kept, float& others) {
+    if (__builtin_expect(__ballot(marked != 0) == 0, 1)) {
+        others += sum_of(e);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const bool hit = marked >> i & 1;
+        kept += hit ? e[i] : 0.f;
+        others += hit ? 0.f : e[i];
+    }
 }
 
-template <class T, bool TAIL, bool BACKWARD>
-__global__ __launch_bounds__(DISTILL_THREADS) void distill_kernel(const DistillArgs a) {
+// What multiplies e in the gradient of a class that was not kept, and of one that was.
+struct Factors { float other, kept; };
+// kept_share: E / Z, over_others: 1 / R or 0 where R is
+__device__ __forceinline__ Factors factors(float mass, float rest, float inv_total, float kept_share, float over_others, float weight) {
+    const bool with_rest = rest > 0.f && over_others != 0.f;
+    return Factors{weight * (mass * inv_total - (with_rest ? rest * kept_share * over_others : 0.f)),
+                   weight * (mass + (with_rest ? rest : 0.f)) * inv_total};
+}
+
+// LDS of a workgroup: a float for each of 16 wavefronts, the record, the marks
+static __host__ __device__ int record_words(int k) { return 16 + 2 * k + 3; }
+
+// A workgroup a row, the row in registers between its maximum, its sums and its gradient.
+template <class T, bool TAIL, int THREADS, int PIECES>
+__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void distill_held_kernel(const DistillArgs a) {
     extern __shared__ int lds[];
-    const int tid = threadIdx.x, lane = tid & 63, k = a.k;
-    const Record record{lds, (float*)lds + 2 * k, (float*)lds + 4 * k};
-    float* const box = (float*)lds + 4 * k + 3;
-    uint32_t* const marks = (uint32_t*)(box + DISTILL_THREADS / 64);
-    const int* const index = record.index + k;
-    const float* const q = record.q + k;
-    const float inv_t = 1.f / a.temperature;
+    const int tid = threadIdx.x, k = a.k;
+    float* const box = (float*)lds;
+    const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
+    uint32_t* const marks = (uint32_t*)lds + record_words(k);
+    const float c = LOG2E / a.temperature;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T* const p = (const T*)a.logits + row * a.ld;
-        const Row<T, DISTILL_THREADS> x(p, a.classes);
-        if (tid < 64) read_record(a, row, lane, record);
-        if (TAIL && !BACKWARD)
-            for (int i = tid; i < (a.classes + 31) / 32; i += DISTILL_THREADS) marks[i] = 0;
-        __syncthreads();
-        if (TAIL && !BACKWARD) {
-            for (int j = tid; j < k; j += DISTILL_THREADS)
-                if (index[j] >= 0) atomicOr(&marks[index[j] >> 5], 1u << (index[j] & 31));
-            __syncthreads();
-        }
-        const float mass = record.sums[0], rest = record.sums[1];
-        float mx = LOWEST, total = 0.f, others = 0.f, ln_total, ln_others = NONE;
-        if constexpr (!BACKWARD) {
-            x.each(tid, [&](float v, int) { mx = fmaxf(mx, v); });
-            mx = group_max<DISTILL_THREADS>(mx, box);
-            float kept = 0.f;
-            x.each(tid, [&](float v, int c) {
-                const float e = exp_of((v - mx) * inv_t);
-                if (TAIL && (marks[c >> 5] >> (c & 31) & 1)) kept += e;
-                else others += e;
-            });
-            others = group_sum<DISTILL_THREADS>(others, box);
-            total = others;
-            if (TAIL) total += group_sum<DISTILL_THREADS>(kept, box);
-            ln_total = logf(total);
-            if (TAIL) ln_others = logf(others);
-            // sum q ln q - sum q ln p
-            float cross = 0.f;
-            for (int j = tid; j < k; j += DISTILL_THREADS)
-                if (index[j] >= 0 && q[j] != 0.f) cross += q[j] * ((up(p[index[j]]) - mx) * inv_t - ln_total);
-            cross = group_sum<DISTILL_THREADS>(cross, box);
-            if (tid == 0) {
-                float loss = record.sums[2] - cross;
-                if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
-                a.loss[row] = total == 0.f ? 0.f : loss * a.temperature * a.temperature;
-                a.state[row * 3] = mx;
-                a.state[row * 3 + 1] = ln_total;
-                a.state[row * 3 + 2] = ln_others;
-            }
-        } else {
-            mx = a.state[row * 3];
-            ln_total = a.state[row * 3 + 1];
-            ln_others = a.state[row * 3 + 2];
-        }
-        if (BACKWARD || a.d_logits) {
-            T* const out = (T*)a.d_logits + row * a.ld_d;
-            const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature;
-            const bool none = weight == 0.f || ln_total == NONE;
-            const bool with_rest = TAIL && rest > 0.f && ln_others > NONE;
-            const float all = mass + (with_rest ? rest : 0.f);
-            // ln(Z / R) beyond 80 belongs to classes of e^-80 and less
-            const float factor = with_rest ? mass - rest * expm1f(fminf(ln_total - ln_others, 80.f)) : mass;
-            float at_kept[(DISTILL_MAX_K + DISTILL_THREADS - 1) / DISTILL_THREADS];
+        const Row<T, THREADS> x(p, a.classes);
+        Held<T, THREADS, PIECES> held;
+        held.load(x, tid);
+        if (TAIL)
+            for (int i = tid; i < mark_words(THREADS * PIECES, PIECE<T>); i += THREADS) marks[i] = 0;
+        if (tid < 64) read_record(a, row, tid, record);
+        group_sync<THREADS>();
+        float at_kept[(DISTILL_MAX_K + THREADS - 1) / THREADS];
+        const int shift = PIECE<T> - x.head;
 #pragma unroll
-            for (int i = 0; i < (DISTILL_MAX_K + DISTILL_THREADS - 1) / DISTILL_THREADS; i++) {
-                const int j = tid + i * DISTILL_THREADS;
-                at_kept[i] = j < k && index[j] >= 0 ? up(p[index[j]]) : 0.f;
-            }
-            __syncthreads();                                     // out may be p
-            x.map(tid, out, [&](float v, int) { return none ? 0.f : weight * factor * exp_of((v - mx) * inv_t - ln_total); });
-            __syncthreads();
+        for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+            const int j = tid + i * THREADS, at = j < k ? record.index[j] : -1;
+            at_kept[i] = at >= 0 ? up(p[at]) : 0.f;
+            if (TAIL && at >= 0) atomicOr(&marks[(at + shift) >> 5], 1u << ((at + shift) & 31));
+        }
+        const float mx = group_max<THREADS>(held.max(x), box);
+        if (TAIL && THREADS == 64) group_sync<THREADS>();
+        float kept = 0.f, others = 0.f;
+        {
+            const float e = __builtin_amdgcn_exp2f((held.one - mx) * c);
+            const bool hit = TAIL && held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1);
+            if (hit) kept = e;
+            else others = e;
+        }
+        held.each(x, [&](float (&v)[PIECE<T>], int piece) {
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) v[e] = __builtin_amdgcn_exp2f((v[e] - mx) * c);
+            if (TAIL) add_piece(v, piece_marks<T>(marks, piece, tid), kept, others);
+            else others += sum_of(v);
+        });
+        others = group_sum<THREADS>(others, box);
+        if (TAIL) kept = group_sum<THREADS>(kept, box);
+        const float total = others + kept, ln_total = logf(total);
+        float cross = 0.f;                                       // sum q ln p
+#pragma unroll
+        for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+            const int j = tid + i * THREADS;
+            if (j < k && record.q[j] != 0.f) cross += record.q[j] * ((at_kept[i] - mx) / a.temperature - ln_total);
+        }
+        cross = group_sum<THREADS>(cross, box);
+        const float mass = record.sums[0], rest = record.sums[1];
+        if (tid == 0) {
+            const float ln_others = TAIL ? logf(others) : NONE;
+            float loss = record.sums[2] - cross;
+            if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
+            a.loss[row] = total == 0.f ? 0.f : loss * a.temperature * a.temperature;
+            a.state[row * 3] = mx;
+            a.state[row * 3 + 1] = ln_total;
+            a.state[row * 3 + 2] = ln_others;
+        }
+        if (a.d_logits) {
+            T* const out = (T*)a.d_logits + row * a.ld_d;
+            const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature, inv_total = 1.f / total;
+            const bool none = weight == 0.f || total == 0.f;
+            const Factors f = factors(mass, TAIL ? rest : 0.f, inv_total, kept * inv_total, others != 0.f ? 1.f / others : 0.f, weight);
+            if (none) held.map(x, tid, out, [&](float) { return 0.f; });
+            else held.map(x, tid, out, [&](float v) { return f.other * __builtin_amdgcn_exp2f((v - mx) * c); });
+            group_sync<THREADS>();
             if (!none)
 #pragma unroll
-                for (int i = 0; i < (DISTILL_MAX_K + DISTILL_THREADS - 1) / DISTILL_THREADS; i++) {
-                    const int j = tid + i * DISTILL_THREADS;
-                    if (j < k && index[j] >= 0) out[index[j]] = (T)(weight * (all * exp_of((at_kept[i] - mx) * inv_t - ln_total) - q[j]));
+                for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+                    const int j = tid + i * THREADS;
+                    if (j < k && record.index[j] >= 0)
+                        out[record.index[j]] = (T)(f.kept * __builtin_amdgcn_exp2f((at_kept[i] - mx) * c) - weight * record.q[j]);
                 }
+        }
+        group_sync<THREADS>();
+    }
+}
+
+// The rows in parts, for rows that are too few or too long for a workgroup each: first every part's maximum and sums and the logits of the
+// kept classes go to the workspace, then every part's workgroup joins them and writes its part of the gradient, the first one the loss.  The second
+// step by itself, from the state, is the backward pass.
+constexpr int PART_THREADS = 256;
+struct Parts {
+    int parts, length;                                           // of every part but the last
+    __host__ __device__ int64_t row_floats(int k) const { return (int64_t)parts * 3 + k; }
+};
+
+template <class T, bool TAIL>
+__global__ __launch_bounds__(PART_THREADS) void distill_part_kernel(const DistillArgs a, const Parts split) {
+    extern __shared__ int lds[];
+    const int tid = threadIdx.x, k = a.k;
+    float* const box = (float*)lds;
+    uint32_t* const marks = (uint32_t*)lds + 16;
+    const float c = LOG2E / a.temperature;
+    for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
+        const int64_t row = job / split.parts;
+        const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
+        const T* const p = (const T*)a.logits + row * a.ld + first;
+        const Row<T, PART_THREADS> x(p, length);
+        float* const out = (float*)a.workspace + row * split.row_floats(k);
+        const int shift = PIECE<T> - x.head;
+        if (TAIL) {
+            for (int i = tid; i < mark_words(x.pieces, PIECE<T>); i += PART_THREADS) marks[i] = 0;
+            __syncthreads();
+        }
+        for (int j = tid; j < k; j += PART_THREADS) {
+            const int64_t at = (int64_t)a.index[row * k + j] - first;
+            if (at < 0 || at >= length) continue;
+            out[split.parts * 3 + j] = up(p[at]);
+            if (TAIL) atomicOr(&marks[(at + shift) >> 5], 1u << ((at + shift) & 31));
+        }
+        if (TAIL) __syncthreads();
+        float m = LOWEST, kept = 0.f, others = 0.f;
+        const int one = x.single(tid);
+        if (one >= 0) {
+            const float v = up(p[one]);
+            m = fmaxf(m, v);
+            const float e = __builtin_amdgcn_exp2f((v - m) * c);
+            if (TAIL && (marks[(one + shift) >> 5] >> ((one + shift) & 31) & 1)) kept = e;
+            else others = e;
+        }
+        for (int i = tid; i < x.pieces; i += PART_THREADS) {
+            float v[PIECE<T>], top = m;
+            unpack(x.body()[i], v, p);
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) top = fmaxf(top, v[e]);
+            const float less = __builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+            kept *= less;
+            others *= less;
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * c);
+            if (TAIL) add_piece(v, piece_marks<T>(marks, i - tid, tid), kept, others);
+            else others += sum_of(v);
+        }
+        const float mx = group_max<PART_THREADS>(m, box);
+        const float less = __builtin_amdgcn_exp2f((m - mx) * c);
+        others = group_sum<PART_THREADS>(others * less, box);
+        if (TAIL) kept = group_sum<PART_THREADS>(kept * less, box);
+        if (tid == 0) {
+            out[part * 3] = mx;
+            out[part * 3 + 1] = kept;
+            out[part * 3 + 2] = others;
         }
         __syncthreads();
     }
 }
 
-int64_t distill_workspace(int64_t, int, int, int) { return 0; }
+template <class T, bool TAIL, bool JOIN>
+__global__ __launch_bounds__(PART_THREADS) void distill_gradient_kernel(const DistillArgs a, const Parts split) {
+    extern __shared__ int lds[];
+    __shared__ float found[4];
+    const int tid = threadIdx.x, lane = tid & 63, k = a.k;
+    const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
+    const float c = LOG2E / a.temperature;
+    for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
+        const int64_t row = job / split.parts;
+        const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
+        const float* const from = (const float*)a.workspace + row * split.row_floats(k);
+        if (tid < 64) {
+            read_record(a, row, lane, record);
+            if (JOIN) {
+                float m = LOWEST, kept = 0.f, others = 0.f;
+                for (int i = lane; i < split.parts; i += 64) m = fmaxf(m, from[i * 3]);
+                m = lanes_max(m);
+                for (int i = lane; i < split.parts; i += 64) {
+                    const float less = __builtin_amdgcn_exp2f((from[i * 3] - m) * c);
+                    kept += from[i * 3 + 1] * less;
+                    others += from[i * 3 + 2] * less;
+                }
+                kept = lanes_sum(kept);
+                others = lanes_sum(others);
+                if (lane == 0) {
+                    found[0] = m;
+                    found[1] = kept + others;
+                    found[2] = kept;
+                    found[3] = others;
+                }
+                if (part == 0) {
+                    const float ln_total = logf(kept + others);
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    float cross = 0.f;
+                    for (int j = lane; j < k; j += 64)
+                        if (record.q[j] != 0.f) cross += record.q[j] * ((from[split.parts * 3 + j] - m) / a.temperature - ln_total);
+                    cross = lanes_sum(cross);
+                    if (lane == 0) {
+                        const float rest = record.sums[1], ln_others = TAIL ? logf(others) : NONE;
+                        float loss = record.sums[2] - cross;
+                        if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
+                        a.loss[row] = kept + others == 0.f ? 0.f : loss * a.temperature * a.temperature;
+                        a.state[row * 3] = m;
+                        a.state[row * 3 + 1] = ln_total;
+                        a.state[row * 3 + 2] = ln_others;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (a.d_logits) {
+            const T* const p = (const T*)a.logits + row * a.ld + first;
+            T* const out = (T*)a.d_logits + row * a.ld_d + first;
+            const Row<T, PART_THREADS> x(p, length);
+            const float mass = record.sums[0], rest = TAIL ? record.sums[1] : 0.f;
+            const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature;
+            float mx, total;
+            Factors f;
+            if (JOIN) {
+                mx = found[0];
+                total = found[1];
+                f = factors(mass, rest, 1.f / total, found[2] / total, found[3] != 0.f ? 1.f / found[3] : 0.f, weight);
+            } else {
+                mx = a.state[row * 3];
+                const float ln_total = a.state[row * 3 + 1], ln_others = a.state[row * 3 + 2];
+                total = expf(ln_total);
+                const bool others = TAIL && ln_others > NONE;
+                f = factors(mass, others ? rest : 0.f, 1.f / total, others ? -expm1f(ln_others - ln_total) : 0.f, others ? expf(-ln_others) : 0.f, weight);
+            }
+            const bool none = weight == 0.f || total == 0.f;
+            float at_kept;
+            int at = -1;
+            static_assert(DISTILL_MAX_K <= PART_THREADS, "an entry a thread");
+            if (tid < k) {
+                const int64_t here = (int64_t)record.index[tid] - first;
+                if (record.index[tid] >= 0 && here >= 0 && here < length) {
+                    at = (int)here;
+                    at_kept = JOIN ? from[split.parts * 3 + tid] : up(p[at]);
+                }
+            }
+            __syncthreads();                                     // out may be p
+            x.map(tid, out, [&](float v, int) { return none ? 0.f : f.other * __builtin_amdgcn_exp2f((v - mx) * c); });
+            __syncthreads();
+            if (at >= 0 && !none) out[at] = (T)(f.kept * __builtin_amdgcn_exp2f((at_kept - mx) * c) - weight * record.q[tid]);
+        }
+        __syncthreads();
+    }
+}
 
-template <bool BACKWARD>
-static hipError_t launch(const DistillArgs& a, hipStream_t s) {
+// Parts so that there are some 1 024 workgroups, of 4 096 classes at least.
+static Parts split_rows(int64_t n, int classes) {
+    const int64_t most = (classes + 4095) / 4096, want = std::max<int64_t>(1, 1024 / n);
+    const int parts = (int)std::max<int64_t>(1, std::min(most, want));
+    const int length = ((classes + parts - 1) / parts + 63) / 64 * 64;
+    return Parts{(classes + length - 1) / length, length};
+}
+
+// A row a workgroup holds it: as many pieces as its registers take, and enough rows to fill the chip.
+static bool held(int64_t n, int classes, int dtype) {
+    const int pieces = classes / (dtype == 0 ? 4 : 8);
+    return pieces <= 1024 * 16 && (n >= 256 || pieces <= 256 * 4);
+}
+
+int64_t distill_workspace(int64_t n, int classes, int k, int dtype) {
+    return held(n, classes, dtype) ? 0 : n * split_rows(n, classes).row_floats(k) * (int64_t)sizeof(float);
+}
+
+template <class T, bool TAIL, int THREADS, int PIECES>
+static hipError_t launch_held(const DistillArgs& a, hipStream_t s) {
+    const int lds = 4 * (record_words(a.k) + (TAIL ? mark_words(THREADS * PIECES, PIECE<T>) : 0));
+    hipLaunchKernelGGL((distill_held_kernel<T, TAIL, THREADS, PIECES>), dim3((unsigned)std::min<int64_t>(a.n, 8192)), dim3(THREADS), lds, s, a);
+    return hipGetLastError();
+}
+
+template <class T, bool TAIL>
+static hipError_t launch_distill_as(const DistillArgs& a, hipStream_t s) {
+    if (held(a.n, a.classes, a.dtype)) {
+        const int pieces = a.classes / PIECE<T>;
+        if (pieces <= 64 * 4) return launch_held<T, TAIL, 64, 4>(a, s);
+        if (pieces <= 256 * 4) return launch_held<T, TAIL, 256, 4>(a, s);
+        if (pieces <= 256 * 8) return launch_held<T, TAIL, 256, 8>(a, s);
+        if (pieces <= 512 * 8) return launch_held<T, TAIL, 512, 8>(a, s);
+        if (pieces <= 512 * 16) return launch_held<T, TAIL, 512, 16>(a, s);
+        return launch_held<T, TAIL, 1024, 16>(a, s);
+    }
+    const Parts split = split_rows(a.n, a.classes);
+    const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 16)), group(PART_THREADS);
+    hipLaunchKernelGGL((distill_part_kernel<T, TAIL>), grid, group, 4 * (16 + (TAIL ? mark_words(split.length / PIECE<T>, PIECE<T>) : 0)), s, a, split);
+    hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, true>), grid, group, 4 * record_words(a.k), s, a, split);
+    return hipGetLastError();
+}
+hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
+    return by_type(a.dtype, [&](auto t) { return a.tail ? launch_distill_as<decltype(t), true>(a, s) : launch_distill_as<decltype(t), false>(a, s); });
+}
+hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {
     return by_type(a.dtype, [&](auto t) {
-        const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 16)), group(DISTILL_THREADS);
-        const int lds = distill_lds(a.k, a.classes, a.tail && !BACKWARD);
-        if (a.tail) hipLaunchKernelGGL((distill_kernel<decltype(t), true, BACKWARD>), grid, group, lds, s, a);
-        else hipLaunchKernelGGL((distill_kernel<decltype(t), false, BACKWARD>), grid, group, lds, s, a);
+        const Parts split = split_rows(a.n, a.classes);
+        const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 16)), group(PART_THREADS);
+        if (a.tail) hipLaunchKernelGGL((distill_gradient_kernel<decltype(t), true, false>), grid, group, 4 * record_words(a.k), s, a, split);
+        else hipLaunchKernelGGL((distill_gradient_kernel<decltype(t), false, false>), grid, group, 4 * record_words(a.k), s, a, split);
         return hipGetLastError();
     });
 }
-hipError_t launch_distill(const DistillArgs& a, hipStream_t s) { return launch<false>(a, s); }
-hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) { return launch<true>(a, s); }
 
 }  // namespace ens

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace ens {
 
 constexpr float LOWEST = -3.402823466e38f;   // running maxima start here: minus infinity less this is minus infinity, not NaN
@@ -119,6 +121,79 @@ struct Row {
         }
     }
 };
+
+// This thread's share of a row in registers, PIECES of 16 bytes a thread at most; places behind the row hold minus infinity.  Addresses are
+// a scalar for all threads and tid * 16, so that pieces take no address registers each.
+template <class T, int THREADS, int PIECES>
+struct Held {
+    uint4 r[PIECES];
+    float one;
+    int at;                                                      // class of `one`, or -1
+    __device__ __forceinline__ void load(const Row<T, THREADS>& x, int tid) {
+        at = x.single(tid);
+        const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
+        const uint32_t mine = (uint32_t)tid * 16u;
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) {
+            const char* const at_i = (const char*)(x.body() + i * THREADS);
+            if ((i + 1) * THREADS <= x.pieces) r[i] = *(const uint4*)(at_i + mine);
+            else {
+                r[i] = make_uint4(none, none, none, none);
+                if (tid < x.pieces - i * THREADS) r[i] = *(const uint4*)(at_i + mine);
+            }
+        }
+        one = at >= 0 ? up(x.p[at]) : NONE;
+    }
+    // f(values of a piece, number of the piece of thread 0) for pieces in reach of the row
+    template <class F>
+    __device__ __forceinline__ void each(const Row<T, THREADS>& x, F f) const {
+#pragma unroll
+        for (int i = 0; i < PIECES; i++)
+            if (i * THREADS < x.pieces) {
+                float v[PIECE<T>];
+                unpack(r[i], v, x.p);
+                f(v, i * THREADS);
+                __builtin_amdgcn_sched_barrier(0);               // pieces mixed with each other take registers that hold rows
+            }
+    }
+    __device__ __forceinline__ float max(const Row<T, THREADS>& x) const {
+        float m = fmaxf(LOWEST, one);
+        each(x, [&](const float (&v)[PIECE<T>], int) {
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) m = fmaxf(m, v[e]);
+        });
+        return m;
+    }
+    // dst[class] = f(value), dst may be the row
+    template <class F>
+    __device__ __forceinline__ void map(const Row<T, THREADS>& x, int tid, T* dst, F f) const {
+        if (at >= 0) dst[at] = (T)f(one);
+        const bool alike = (((uintptr_t)dst - (uintptr_t)x.p) & 15u) == 0;
+        const uint32_t mine = (uint32_t)tid * 16u;
+        each(x, [&](float (&v)[PIECE<T>], int piece) {
+            if (tid >= x.pieces - piece) return;
+            char* const to = (char*)(dst + x.head + piece * PIECE<T>);
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++) v[e] = f(v[e]);
+            if (alike) *(uint4*)(to + mine) = pack(v, x.p);
+            else
+#pragma unroll
+                for (int e = 0; e < PIECE<T>; e++) *(T*)(to + mine + e * sizeof(T)) = (T)v[e];
+        });
+    }
+};
+template <int N>
+__device__ __forceinline__ float sum_of(const float (&v)[N]) {
+    if constexpr (N == 8) return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    else return (v[0] + v[1]) + (v[2] + v[3]);
+}
+
+// Between the wavefronts of a workgroup, or the lanes of the only one.
+template <int THREADS>
+__device__ __forceinline__ void group_sync() {
+    if constexpr (THREADS > 64) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
 
 // Over a workgroup; `box`: a float for each of its wavefronts.  Every thread gets the result, added or compared in the same order.
 template <int THREADS>
