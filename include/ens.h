@@ -319,7 +319,7 @@ double ens_last_ms(const ens_handle* h);
  *   ld     elements between the starts of two rows, at least the row's length; rows need no more
  *          alignment than their elements
  * Arrays without an ld are contiguous.  n = 0 does nothing.  ENS_E_INVALID for what no call may say,
- * ENS_E_UNSUPPORTED beyond the stated limits.
+ * ENS_E_UNSUPPORTED beyond the stated limits, and for temperatures outside 2^-20 .. 2^20.
  */
 enum { ENS_SCORE_SOFTMAX = 0, ENS_SCORE_SIGMOID = 1 };
 typedef struct {

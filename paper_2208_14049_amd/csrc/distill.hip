@@ -129,7 +129,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) vo
     float* const box = (float*)lds;
     const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
     uint32_t* const marks = (uint32_t*)lds + record_words(k);
-    const float c = LOG2E / a.temperature;
+    const float cooling = 1.f / a.temperature;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T* const p = (const T*)a.logits + row * a.ld;
         const Row<T, THREADS> x(p, a.classes);
@@ -149,22 +149,23 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) vo
         }
         const float mx = group_max<THREADS>(held.max(x), box);
         if (TAIL && THREADS == 64) group_sync<THREADS>();
+        const Exp power(mx, cooling);
         float kept = 0.f, others = 0.f;
         {
-            const float e = __builtin_amdgcn_exp2f((held.one - mx) * c);
+            const float e = power(held.one);
             const bool hit = TAIL && held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1);
             if (hit) kept = e;
             else others = e;
         }
         held.each(x, [&](float (&v)[PIECE<T>], int piece) {
 #pragma unroll
-            for (int e = 0; e < PIECE<T>; e++) v[e] = __builtin_amdgcn_exp2f((v[e] - mx) * c);
+            for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
             if (TAIL) add_piece(v, piece_marks<T>(marks, piece, tid), kept, others);
             else others += sum_of(v);
         });
         others = group_sum<THREADS>(others, box);
         if (TAIL) kept = group_sum<THREADS>(kept, box);
-        const float total = others + kept, ln_total = logf(total);
+        const float total = others + kept, off = power.off(), ln_total = logf(total * off);
         float cross = 0.f;                                       // sum q ln p
 #pragma unroll
         for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) vo
         cross = group_sum<THREADS>(cross, box);
         const float mass = record.sums[0], rest = record.sums[1];
         if (tid == 0) {
-            const float ln_others = TAIL ? logf(others) : NONE;
+            const float ln_others = TAIL ? logf(others * off) : NONE;
             float loss = record.sums[2] - cross;
             if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
             a.loss[row] = total == 0.f ? 0.f : loss * a.temperature * a.temperature;
@@ -188,14 +189,14 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) vo
             const bool none = weight == 0.f || total == 0.f;
             const Factors f = factors(mass, TAIL ? rest : 0.f, inv_total, kept * inv_total, others != 0.f ? 1.f / others : 0.f, weight);
             if (none) held.map(x, tid, out, [&](float) { return 0.f; });
-            else held.map(x, tid, out, [&](float v) { return f.other * __builtin_amdgcn_exp2f((v - mx) * c); });
+            else held.map(x, tid, out, [&](float v) { return f.other * power(v); });
             group_sync<THREADS>();
             if (!none)
 #pragma unroll
                 for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
                     const int j = tid + i * THREADS;
                     if (j < k && record.index[j] >= 0)
-                        out[record.index[j]] = (T)(f.kept * __builtin_amdgcn_exp2f((at_kept[i] - mx) * c) - weight * record.q[j]);
+                        out[record.index[j]] = (T)(f.kept * power(at_kept[i]) - weight * record.q[j]);
                 }
         }
         group_sync<THREADS>();
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(PART_THREADS) void distill_part_kernel(const Distil
     const int tid = threadIdx.x, k = a.k;
     float* const box = (float*)lds;
     uint32_t* const marks = (uint32_t*)lds + 16;
-    const float c = LOG2E / a.temperature;
+    const float cooling = 1.f / a.temperature;
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = job / split.parts;
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(PART_THREADS) void distill_part_kernel(const Distil
         if (one >= 0) {
             const float v = up(p[one]);
             m = fmaxf(m, v);
-            const float e = __builtin_amdgcn_exp2f((v - m) * c);
+            const float e = Exp(m, cooling)(v);
             if (TAIL && (marks[(one + shift) >> 5] >> ((one + shift) & 31) & 1)) kept = e;
             else others = e;
         }
@@ -250,17 +251,19 @@ __global__ __launch_bounds__(PART_THREADS) void distill_part_kernel(const Distil
             unpack(x.body()[i], v, p);
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) top = fmaxf(top, v[e]);
-            const float less = __builtin_amdgcn_exp2f((m - top) * c);
+            const Exp power(top, cooling);
+            const float less = Exp(m, cooling).to(power);
             m = top;
             kept *= less;
             others *= less;
 #pragma unroll
-            for (int e = 0; e < PIECE<T>; e++) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * c);
+            for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
             if (TAIL) add_piece(v, piece_marks<T>(marks, i - tid, tid), kept, others);
             else others += sum_of(v);
         }
         const float mx = group_max<PART_THREADS>(m, box);
-        const float less = __builtin_amdgcn_exp2f((m - mx) * c);
+        const Exp power(mx, cooling);
+        const float less = Exp(m, cooling).to(power) * power.off();
         others = group_sum<PART_THREADS>(others * less, box);
         if (TAIL) kept = group_sum<PART_THREADS>(kept * less, box);
         if (tid == 0) {
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(PART_THREADS) void distill_gradient_kernel(const Di
     __shared__ float found[4];
     const int tid = threadIdx.x, lane = tid & 63, k = a.k;
     const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
-    const float c = LOG2E / a.temperature;
+    const float cooling = 1.f / a.temperature;
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = job / split.parts;
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
@@ -290,7 +293,8 @@ __global__ __launch_bounds__(PART_THREADS) void distill_gradient_kernel(const Di
                 for (int i = lane; i < split.parts; i += 64) m = fmaxf(m, from[i * 3]);
                 m = lanes_max(m);
                 for (int i = lane; i < split.parts; i += 64) {
-                    const float less = __builtin_amdgcn_exp2f((from[i * 3] - m) * c);
+                    const Exp power(m, cooling);
+                    const float less = __builtin_amdgcn_exp2f((from[i * 3] - m) * power.c);
                     kept += from[i * 3 + 1] * less;
                     others += from[i * 3 + 2] * less;
                 }
@@ -353,9 +357,11 @@ __global__ __launch_bounds__(PART_THREADS) void distill_gradient_kernel(const Di
                 }
             }
             __syncthreads();                                     // out may be p
-            x.map(tid, out, [&](float v, int) { return none ? 0.f : f.other * __builtin_amdgcn_exp2f((v - mx) * c); });
+            const Exp power(mx, cooling);
+            const float other = f.other * power.off(), own = f.kept * power.off();
+            x.map(tid, out, [&](float v, int) { return none ? 0.f : other * power(v); });
             __syncthreads();
-            if (at >= 0 && !none) out[at] = (T)(f.kept * __builtin_amdgcn_exp2f((at_kept - mx) * c) - weight * record.q[tid]);
+            if (at >= 0 && !none) out[at] = (T)(own * power(at_kept) - weight * record.q[tid]);
         }
         __syncthreads();
     }

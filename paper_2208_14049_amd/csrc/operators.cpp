@@ -16,6 +16,8 @@ static bool row_buffer(const void* p, int dtype, int64_t n, int64_t len, int64_t
 }
 static bool words(const void* p) { return p && aligned(p, 4); }
 static bool words_or_null(const void* p) { return aligned(p, 4); }
+// Temperatures at which every product of a logit is in reach of fp32 (Exp in rows.h).
+static int temperature_status(float t) { return !(t > 0.f && std::isfinite(t)) ? ENS_E_INVALID : t < 0x1p-20f || t > 0x1p20f ? ENS_E_UNSUPPORTED : ENS_OK; }
 static int status(hipError_t e) { return e == hipSuccess ? ENS_OK : e == hipErrorNoDevice ? ENS_E_NODEVICE : ENS_E_HIP; }
 
 extern "C" {
@@ -114,7 +116,7 @@ int ens_top(const void* values, int32_t dtype, int64_t ld, int64_t n, int32_t cl
     const int64_t want = ens_top_workspace(n, classes, k, dtype);
     if (want < 0) return (int)want;
     if (form != ENS_TOP_VALUE && form != ENS_TOP_LOG && form != ENS_TOP_LOG_SOFTMAX) return ENS_E_INVALID;
-    if (form == ENS_TOP_LOG_SOFTMAX && !(temperature > 0.f && std::isfinite(temperature))) return ENS_E_INVALID;
+    if (form == ENS_TOP_LOG_SOFTMAX && temperature_status(temperature) != ENS_OK) return temperature_status(temperature);
     if (n == 0) return ENS_OK;
     if (!row_buffer(values, dtype, n, classes, ld) || !words(index) || !words(value)) return ENS_E_INVALID;
     if (want > 0 && (!workspace || !aligned(workspace, 8) || workspace_bytes < want)) return ENS_E_INVALID;
@@ -140,7 +142,7 @@ static int distill_args(const void* logits, int32_t dtype, int64_t ld, int64_t n
                         int32_t k, float temperature, int32_t tail, const float* row_weights, DistillArgs* a) {
     const int rc = distill_sizes(n, classes, k, dtype, tail);
     if (rc != ENS_OK) return rc;
-    if (!(temperature > 0.f && std::isfinite(temperature))) return ENS_E_INVALID;
+    if (temperature_status(temperature) != ENS_OK) return temperature_status(temperature);
     *a = DistillArgs{};
     if (n == 0) return ENS_OK;
     if (!row_buffer(logits, dtype, n, classes, ld) || !words(index) || !words(log_probs) || !words_or_null(row_weights)) return ENS_E_INVALID;

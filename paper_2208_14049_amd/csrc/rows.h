@@ -52,6 +52,28 @@ __device__ __forceinline__ uint4 pack(const float (&f)[8], const _Float16*) {
     return __builtin_bit_cast(uint4, __builtin_convertvector(v, half8));
 }
 
+// e^((x - m) s) for many x, m their maximum, as one multiply-add and the hardware's power of two (off by one unit): 2^(x c - b) with c = s log2 e
+// and b = m c rounded.  The product x c is not rounded, so that a term is off by what c is (2^-24 of the distance x - m, twice) however
+// large x is; b's rounding is a factor 2^rest that all terms share: ratios of them need nothing, sums are multiplied by off.  |rest| is 64 at
+// most up to a product of 2^31.  Beyond that neighbouring values lie 2^7 / c apart and more, so that no value but m counts whatever c is: a power of
+// two makes the product exact and keeps it in range.
+struct Exp {
+    float c, b, m;
+    __device__ __forceinline__ Exp(float max, float s) : m(max) {
+        c = s * LOG2E;
+        b = m * c;
+        if (!(fabsf(b) <= 0x1p31f)) {
+            c = __uint_as_float((127u + 40u + 127u - (__float_as_uint(m) >> 23 & 0xFFu)) << 23);   // m c = 2^40 to 2^41
+            b = m * c;
+        }
+    }
+    __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, c, -b)); }
+    __device__ __forceinline__ float rest() const { return fmaf(m, c, -b); }
+    __device__ __forceinline__ float off() const { return __builtin_amdgcn_exp2f(-rest()); }
+    // what takes sums of these terms to sums of those of a larger maximum
+    __device__ __forceinline__ float to(const Exp& larger) const { return __builtin_amdgcn_exp2f(fmaf(m, larger.c, -larger.b) - rest()); }
+};
+
 // e^d for d <= 0.  The argument is a difference to a maximum, so that its product with log2 e is off by 2^-24 of itself, and the
 // hardware's power of two by one unit more.
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }

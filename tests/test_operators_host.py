@@ -85,6 +85,7 @@ INVALID = [
 UNSUPPORTED = [
     (route, dict(members=513, ld=513)), (route, dict(members=64, ld=64, k=33)), (route, dict(members=130, ld=130, groups=65, groups_kept=65)),
     (combine, dict(members=65, logits=pointers(*[P] * 65))), (combine, dict(k=65)), (combine, dict(classes=(1 << 24) + 1, ld=1 << 25)),
+    (top, dict(temperature=2.0 ** -21)), (top, dict(temperature=2.0 ** 21)), (distill, dict(temperature=1e-9)), (distill_backward, dict(temperature=1e9)),
     (top, dict(k=129, classes=1000, ld=1000)), (top, dict(classes=(1 << 24) + 1, ld=1 << 25)),
     (distill, dict(k=257)), (distill, dict(classes=(1 << 24) + 1, ld=1 << 25)), (distill, dict(classes=(1 << 18) + 1, ld=1 << 19, tail=1)),
     (distill_backward, dict(classes=(1 << 18) + 1, ld=1 << 19, ld_d=1 << 19, tail=1)),
