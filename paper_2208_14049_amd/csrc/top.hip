@@ -1,9 +1,12 @@
 // The k best classes of a row, the lowest class first among equal values, NaN below everything.
 //
-// Values are compared as 32-bit keys whose order is theirs.  Of the threads' own maxima the k-th largest, t, is a bound: k values at least are no
-// smaller.  What is larger than t (some k (1 + k / threads) values where the row is in no order) is collected in LDS and ranked by comparing every pair,
-// 32 bits of key before the class.  Where too many are larger the bound is raised by halving its distance to the maximum, and where equal
-// ones at the bound are too many the lowest classes among them are found walking the row in order.
+// A workgroup (a wavefront for short rows) holds the row in registers.  Of the maxima of 64 to 256 groups of its lanes the k-th largest, t, is a
+// bound: k values at least are no smaller.  What is not smaller (some k (1 + k / groups) values where the row is in no order) is collected in
+// LDS and ranked by comparing every pair, as 64-bit keys: 32 bits in the order of the values, then the class.  Everything is one look at the row for
+// the maxima, a second one at the pieces that hold something, and a third for the sum of a softmax.
+// Where too many values are no smaller than t (equal ones, most of the row masked, the large ones in few lanes), or too few (NaN), the bound is found
+// by halving, over the row in memory.
+// Few or long rows go in parts, each part's best to the workspace, and a second launch chooses among them.
 #include <algorithm>
 
 #include "operators.h"
@@ -12,7 +15,9 @@
 namespace ens {
 
 enum { TOP_VALUE = 0, TOP_LOG = 1, TOP_LOG_SOFTMAX = 2 };
-constexpr int TOP_THREADS = 256, TOP_ROOM = 1024;
+constexpr int TOP_ROOM = 1024, TOP_WAVE_ROOM = 256;     // candidates in LDS
+constexpr int TOP_WAVE_K = 32;                          // for which the 64 lanes of a wavefront are groups enough
+constexpr int JOIN_THREADS = 256, JOIN_KEYS = 2048;     // keys of a row's parts: 8 a thread, so that 128 threads' keys have room
 
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);                 // both zeros are one
@@ -22,119 +27,312 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     if (key == 0u) return __uint_as_float(0x7FC00000u);
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
+// Larger value first, then lower class; no key is 0.
+__device__ __forceinline__ uint64_t key_of(float v, int c) { return (uint64_t)key_of(v) << 32 | (0xFFFFFFFFu - (uint32_t)c); }
 
 template <int THREADS>
-__device__ __forceinline__ int group_count(int v, int* box) {
+__device__ __forceinline__ int group_count(int v, float* box) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0;
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = __int_as_float(v);
+        __syncthreads();
+        v = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; w++) v += box[w];
+        for (int w = 0; w < THREADS / 64; w++) v += __float_as_int(box[w]);
+    }
     return v;
 }
 
-template <class T>
-__global__ __launch_bounds__(TOP_THREADS) void top_kernel(const TopArgs a) {
-    __shared__ uint64_t found[TOP_ROOM];
-    __shared__ uint32_t maxima[TOP_THREADS], bound;
-    __shared__ float box[TOP_THREADS / 64];
-    __shared__ int ibox[TOP_THREADS / 64], count;
+// The best k of a row that holds k values at least, by halving the interval of keys that the k-th lies in: into found[0 .. ), k of them at least and
+// `room` at most.  Returns how many.
+template <class T, int THREADS>
+__device__ __attribute__((noinline)) int halve(const T* p, int len, int base, int k, int room, uint64_t* found, int* count, float* box) {
+    const int tid = threadIdx.x;
+    const Row<T, THREADS> x(p, len);
+    auto larger = [&](uint32_t than) {
+        int c = 0;
+        x.each(tid, [&](float v, int) { c += key_of(v) > than; });
+        return group_count<THREADS>(c, box);
+    };
+    // k values at least are not smaller than t, fewer than k are larger than high
+    uint32_t t = 0, high = 0xFFFFFFFFu;
+    int above = larger(t);
+    if (above >= k && above > room) {
+        while (high - t > 1u) {
+            const uint32_t middle = t + (high - t) / 2;
+            const int c = larger(middle);
+            if (c >= k) t = middle, above = c;
+            else high = middle;
+            if (c >= k && c <= room) break;
+        }
+        if (above > room) {                                      // the k-th value is `high` itself
+            t = high;
+            above = larger(t);
+        }
+    }
+    group_sync<THREADS>();
+    if (tid == 0) *count = 0;
+    group_sync<THREADS>();
+    x.each(tid, [&](float v, int c) {
+        const uint32_t key = key_of(v);
+        if (key > t) found[atomicAdd(count, 1)] = (uint64_t)key << 32 | (0xFFFFFFFFu - (uint32_t)(base + c));
+    });
+    group_sync<THREADS>();
+    int have = above;
+    // and the lowest of those that equal t, in order
+    for (int c0 = 0; have < k && c0 < len; c0 += THREADS) {
+        const int c = c0 + tid;
+        const bool hit = c < len && key_of(up(p[c])) == t;
+        const unsigned long long mask = __ballot(hit);
+        int at = have + __popcll(mask & ((1ull << (tid & 63)) - 1));
+        if constexpr (THREADS > 64) {
+            __syncthreads();
+            if ((tid & 63) == 0) box[tid >> 6] = __int_as_float(__popcll(mask));
+            __syncthreads();
+            for (int w = 0; w < THREADS / 64; w++) {
+                if (w < tid >> 6) at += __float_as_int(box[w]);
+                have += __float_as_int(box[w]);
+            }
+        } else have += __popcll(mask);
+        if (hit && at < k) found[at] = (uint64_t)t << 32 | (0xFFFFFFFFu - (uint32_t)(base + c));
+    }
+    group_sync<THREADS>();
+    return above < k ? k : above;
+}
+
+// Calls f(rank, key) for the best k of `have` different keys in LDS, in no order.
+template <int THREADS, class F>
+__device__ __forceinline__ void rank_keys(const uint64_t* found, int have, int k, F f) {
+    for (int i = threadIdx.x; i < have; i += THREADS) {
+        const uint64_t one = found[i];
+        int at = 0;
+#pragma unroll 4
+        for (int o = 0; o < have; o++) at += found[o] > one;
+        if (at < k) f(at, one);
+    }
+}
+
+struct TopParts {
+    int parts, length;                                           // classes of every part but the last
+    // of the workspace, in 8 bytes: k keys for each part of each row, then a maximum and a sum for each
+    __host__ __device__ int64_t keys(int64_t n, int k) const { return n * parts * k; }
+    __host__ __device__ int64_t bytes(int64_t n, int k) const { return parts == 1 ? 0 : 8 * (keys(n, k) + n * parts); }
+};
+
+template <class T, int THREADS, int PIECES, bool LSE>
+__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
+    constexpr int ROOM = THREADS == 64 ? TOP_WAVE_ROOM : TOP_ROOM, MOST = THREADS < 256 ? THREADS : 256;
+    __shared__ uint64_t found[ROOM];
+    __shared__ __align__(16) float maxima[MOST];
+    __shared__ float box[16];
+    __shared__ uint32_t bound;
+    __shared__ int count;
     const int tid = threadIdx.x, k = a.k;
+    const int groups = THREADS == 64 || k <= 32 ? 64 : k <= 64 ? 128 : 256;    // twice k, so that few values exceed the bound
+    for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
+        const int64_t row = split.parts == 1 ? job : job / split.parts;
+        const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
+        const T* const p = (const T*)a.values + row * a.ld + first;
+        const Row<T, THREADS> x(p, length);
+        Held<T, THREADS, PIECES> held;
+        held.load(x, tid);
+        const float own = held.max(x);                           // LOWEST for nothing but minus infinity
+        float folded = own;
+        for (int o = 1; o < THREADS / groups; o <<= 1) folded = fmaxf(folded, __shfl_xor(folded, o, 64));
+        const int member = THREADS / groups;
+        if (tid % member == 0) maxima[tid / member] = folded;
+        if (tid == 0) {
+            count = 0;
+            bound = 0;
+        }
+        group_sync<THREADS>();
+        if (tid < groups) {
+            const float mine = maxima[tid];
+            int no_smaller = 0;
+            for (int i = 0; i < groups; i += 4) {
+                const float4 m = *(const float4*)&maxima[i];
+                no_smaller += (m.x >= mine) + (m.y >= mine) + (m.z >= mine) + (m.w >= mine);
+            }
+            // the k-th largest is the largest that k of them reach
+            const float reached = lanes_max(no_smaller >= k ? mine : LOWEST);
+            if ((tid & 63) == 0) atomicMax(&bound, key_of(reached));
+        }
+        float mx = LOWEST, sum = 0.f;
+        if (LSE) {
+            mx = group_max<THREADS>(own, box);
+            const Exp power(mx, a.inv_temperature);
+            held.each(x, [&](const float (&v)[PIECE<T>], int) {
+                float e[PIECE<T>];
+#pragma unroll
+                for (int i = 0; i < PIECE<T>; i++) e[i] = power(v[i]);
+                sum += sum_of(e);
+            });
+            sum = group_sum<THREADS>(sum + power(held.one), box) * power.off();
+        }
+        group_sync<THREADS>();
+        const float t = value_of(bound);
+        if (held.at >= 0 && held.one >= t) {
+            const int at = atomicAdd(&count, 1);
+            if (at < ROOM) found[at] = key_of(held.one, first + held.at);
+        }
+        held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
+            float most = v[0];
+#pragma unroll
+            for (int e = 1; e < PIECE<T>; e++) most = fmaxf(most, v[e]);
+            if (!(most >= t) || tid >= x.pieces - piece) return;
+#pragma unroll
+            for (int e = 0; e < PIECE<T>; e++)
+                if (v[e] >= t) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < ROOM) found[at] = key_of(v[e], first + x.head + (piece + tid) * PIECE<T> + e);
+                }
+        });
+        group_sync<THREADS>();
+        int have = count;
+        const int want = min(k, length);
+        if (have > ROOM || have < want) have = halve<T, THREADS>(p, length, first, want, ROOM, found, &count, box);
+        if (split.parts == 1) {
+            const float shift = LSE ? sum == 0.f ? 0.f : logf(sum) : 0.f;      // a row of minus infinities keeps them
+            rank_keys<THREADS>(found, have, k, [&](int at, uint64_t key) {
+                const float v = value_of((uint32_t)(key >> 32));
+                a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+                a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
+            });
+        } else {
+            uint64_t* const out = (uint64_t*)a.workspace + job * k;
+            rank_keys<THREADS>(found, have, want, [&](int at, uint64_t key) { out[at] = key; });
+            for (int i = want + tid; i < k; i += THREADS) out[i] = 0;
+            if (tid == 0) ((float2*)a.workspace)[split.keys(a.n, k) + job] = make_float2(mx, sum);
+        }
+        group_sync<THREADS>();
+    }
+}
+
+// Among the keys that the parts of a row left.  They are dealt to the threads in turn, so that a part's best are with as many threads; k of
+// the threads' maxima reach the k-th largest of them, and what those threads hold has room.
+template <bool LSE>
+__global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(const TopArgs a, const TopParts split) {
+    __shared__ uint64_t found[JOIN_KEYS / JOIN_THREADS * TOP_MAX_K], maxima[JOIN_THREADS];
+    __shared__ uint64_t bound;
+    __shared__ int count;
+    const int tid = threadIdx.x, lane = tid & 63, k = a.k;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const T* const p = (const T*)a.values + row * a.ld;
-        const Row<T, TOP_THREADS> x(p, a.classes);
-        uint32_t best = 0;
-        float mx = LOWEST;
-        x.each(tid, [&](float v, int) { best = max(best, key_of(v)); mx = fmaxf(mx, v); });
-        float shift = 0.f;
-        if (a.form == TOP_LOG_SOFTMAX) {
-            mx = group_max<TOP_THREADS>(mx, box);
-            float sum = 0.f;
-            x.each(tid, [&](float v, int) { sum += exp_of((v - mx) * a.inv_temperature); });
-            sum = group_sum<TOP_THREADS>(sum, box);
-            shift = sum == 0.f ? 0.f : logf(sum);               // a row of minus infinities keeps them
+        const uint64_t* const in = (const uint64_t*)a.workspace + row * split.parts * k;
+        uint64_t mine[JOIN_KEYS / JOIN_THREADS], best = 0;
+#pragma unroll
+        for (int i = 0; i < JOIN_KEYS / JOIN_THREADS; i++) {
+            const int at = i * JOIN_THREADS + tid;
+            mine[i] = at < split.parts * k ? in[at] : 0;
+            best = mine[i] > best ? mine[i] : best;
         }
         maxima[tid] = best;
-        if (tid == 0) count = 0;
-        __syncthreads();
-        int rank = 0;
-        for (int i = 0; i < TOP_THREADS; i++) rank += maxima[i] > best || (maxima[i] == best && i < tid);
-        if (rank == k - 1) bound = best;
-        if (rank == 0) ibox[0] = (int)best;
-        __syncthreads();
-        uint32_t t = bound, high = (uint32_t)ibox[0];
-        auto larger = [&](uint32_t than) {
-            int c = 0;
-            x.each(tid, [&](float v, int) { c += key_of(v) > than; });
-            return group_count<TOP_THREADS>(c, ibox);
-        };
-        int above = larger(t);
-        if (above > TOP_ROOM) {                                  // k values at least are larger than t, none is larger than high
-            while (high - t > 1u) {
-                const uint32_t middle = t + (high - t) / 2;
-                const int c = larger(middle);
-                if (c >= k) t = middle, above = c;
-                else high = middle;
-                if (c >= k && c <= TOP_ROOM) break;
-            }
-            if (above > TOP_ROOM) {                              // the k-th value is `high` itself
-                t = high;
-                above = larger(t);
-            }
+        if (tid == 0) {
+            count = 0;
+            bound = 0;
         }
-        int equal = 0;
-        x.each(tid, [&](float v, int) { equal += key_of(v) == t; });
-        equal = group_count<TOP_THREADS>(equal, ibox);
-        const bool all = above + equal <= TOP_ROOM;
-        x.each(tid, [&](float v, int c) {
-            const uint32_t key = key_of(v);
-            if (key > t || (all && key == t)) {
-                const int at = atomicAdd(&count, 1);
-                found[at] = (uint64_t)key << 32 | (0xFFFFFFFFu - (uint32_t)c);
-            }
+        float mx = LOWEST, sum = 0.f;
+        if (LSE) {                                               // every wavefront for itself
+            const float2* const from = (const float2*)a.workspace + split.keys(a.n, k) + row * split.parts;
+            for (int i = lane; i < split.parts; i += 64) mx = fmaxf(mx, from[i].x);
+            mx = lanes_max(mx);
+            const Exp power(mx, a.inv_temperature);
+            for (int i = lane; i < split.parts; i += 64) sum += from[i].y * __builtin_amdgcn_exp2f((from[i].x - mx) * power.c);
+            sum = lanes_sum(sum);
+        }
+        __syncthreads();
+        int larger = 0;
+#pragma unroll 4
+        for (int i = 0; i < JOIN_THREADS; i++) larger += maxima[i] > best;
+        if (larger == k - 1 && best) bound = best;               // (fewer than k threads with keys: all keys)
+        __syncthreads();
+        const uint64_t t = bound ? bound : 1;
+#pragma unroll
+        for (int i = 0; i < JOIN_KEYS / JOIN_THREADS; i++)
+            if (mine[i] >= t) found[atomicAdd(&count, 1)] = mine[i];
+        __syncthreads();
+        const float shift = LSE ? sum == 0.f ? 0.f : logf(sum) : 0.f;
+        rank_keys<JOIN_THREADS>(found, count, k, [&](int at, uint64_t key) {
+            const float v = value_of((uint32_t)(key >> 32));
+            a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+            a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
         });
-        __syncthreads();
-        int have = count;
-        if (!all && above < k) {                                 // the lowest of the equal ones, in order
-            for (int c0 = 0; have < k && c0 < a.classes; c0 += TOP_THREADS) {
-                const int c = c0 + tid;
-                const bool hit = c < a.classes && key_of(up(p[c])) == t;
-                const unsigned long long mask = __ballot(hit);
-                __syncthreads();
-                if ((tid & 63) == 0) ibox[tid >> 6] = __popcll(mask);
-                __syncthreads();
-                int at = have + __popcll(mask & ((1ull << (tid & 63)) - 1));
-                for (int w = 0; w < TOP_THREADS / 64; w++) {
-                    if (w < tid >> 6) at += ibox[w];
-                    have += ibox[w];
-                }
-                if (hit && at < k) found[at] = (uint64_t)t << 32 | (0xFFFFFFFFu - (uint32_t)c);
-            }
-            have = min(have, k);
-            __syncthreads();
-        }
-        for (int i = tid; i < have; i += TOP_THREADS) {
-            const uint64_t one = found[i];
-            int at = 0;
-            for (int o = 0; o < have; o++) at += found[o] > one;
-            if (at < k) {
-                const float v = value_of((uint32_t)(one >> 32));
-                a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)one);
-                a.value[row * k + at] = a.form == TOP_VALUE ? v : a.form == TOP_LOG ? logf(v) : (v - mx) * a.inv_temperature - shift;
-            }
-        }
         __syncthreads();
     }
 }
 
-int64_t top_workspace(int64_t, int, int, int) { return 0; }
+// Rows that are too long for the keys of their parts: a workgroup walks each in memory.
+template <class T, bool LSE>
+__global__ __launch_bounds__(1024) void top_long_kernel(const TopArgs a) {
+    __shared__ uint64_t found[TOP_ROOM];
+    __shared__ float box[16];
+    __shared__ int count;
+    const int tid = threadIdx.x, k = a.k;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const T* const p = (const T*)a.values + row * a.ld;
+        float mx = LOWEST, shift = 0.f;
+        if (LSE) {
+            const Row<T, 1024> x(p, a.classes);
+            x.each(tid, [&](float v, int) { mx = fmaxf(mx, v); });
+            mx = group_max<1024>(mx, box);
+            const Exp power(mx, a.inv_temperature);
+            float sum = 0.f;
+            x.each(tid, [&](float v, int) { sum += power(v); });
+            sum = group_sum<1024>(sum, box);
+            shift = sum == 0.f ? 0.f : logf(sum * power.off());
+        }
+        const int have = halve<T, 1024>(p, a.classes, 0, k, TOP_ROOM, found, &count, box);
+        rank_keys<1024>(found, have, k, [&](int at, uint64_t key) {
+            const float v = value_of((uint32_t)(key >> 32));
+            a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+            a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
+        });
+        __syncthreads();
+    }
+}
+
+// How a call's rows are cut; parts 0: too long.
+static TopParts split_top(int64_t n, int classes, int k, int dtype) {
+    const int piece = dtype == 0 ? 4 : 8, pieces = classes / piece;
+    const int most = std::max(1, JOIN_KEYS / k);
+    int parts = 1;
+    if (n < 256 && pieces > 1024) parts = std::min<int64_t>({(pieces + 511) / 512, most, std::max<int64_t>(1, 1024 / n)});
+    if (pieces > 16384) parts = std::max(parts, (pieces + 8191) / 8192);
+    if (parts > most) return TopParts{0, 0};
+    const int length = ((classes + parts - 1) / parts + 63) / 64 * 64;
+    return TopParts{(classes + length - 1) / length, length};
+}
+
+int64_t top_workspace(int64_t n, int classes, int k, int dtype) { return split_top(n, classes, k, dtype).parts ? split_top(n, classes, k, dtype).bytes(n, k) : 0; }
+
+template <class T, int THREADS, int PIECES>
+static void launch_top_held(const TopArgs& a, const TopParts& split, hipStream_t s) {
+    const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 14)), group(THREADS);
+    if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_held_kernel<T, THREADS, PIECES, true>), grid, group, 0, s, a, split);
+    else hipLaunchKernelGGL((top_held_kernel<T, THREADS, PIECES, false>), grid, group, 0, s, a, split);
+}
 
 hipError_t launch_top(const TopArgs& a, hipStream_t s) {
+    const TopParts split = split_top(a.n, a.classes, a.k, a.dtype);
     return by_type(a.dtype, [&](auto t) {
-        hipLaunchKernelGGL((top_kernel<decltype(t)>), dim3((unsigned)std::min<int64_t>(a.n, 1 << 16)), dim3(TOP_THREADS), 0, s, a);
+        typedef decltype(t) T;
+        const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 14));
+        if (split.parts == 0) {
+            if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_long_kernel<T, true>), rows, dim3(1024), 0, s, a);
+            else hipLaunchKernelGGL((top_long_kernel<T, false>), rows, dim3(1024), 0, s, a);
+            return hipGetLastError();
+        }
+        const int pieces = split.length / PIECE<T>;
+        if (pieces <= 64 * 4 && a.k <= TOP_WAVE_K) launch_top_held<T, 64, 4>(a, split, s);
+        else if (pieces <= 256 * 4) launch_top_held<T, 256, 4>(a, split, s);
+        else if (pieces <= 512 * 8) launch_top_held<T, 512, 8>(a, split, s);
+        else if (pieces <= 512 * 16) launch_top_held<T, 512, 16>(a, split, s);
+        else launch_top_held<T, 1024, 16>(a, split, s);
+        if (split.parts > 1) {
+            if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_join_kernel<true>), rows, dim3(JOIN_THREADS), 0, s, a, split);
+            else hipLaunchKernelGGL((top_join_kernel<false>), rows, dim3(JOIN_THREADS), 0, s, a, split);
+        }
         return hipGetLastError();
     });
 }
