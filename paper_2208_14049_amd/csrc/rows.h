@@ -144,6 +144,9 @@ struct Row {
     }
 };
 
+// The compiler takes u for a new value from here on: it would keep the unpacked values of a row from one use of it to the next, in twice the registers.
+__device__ __forceinline__ void renew(uint4& u) { asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
+
 // This thread's share of a row in registers, PIECES of 16 bytes a thread at most; places behind the row hold minus infinity.  Addresses are
 // a scalar for all threads and tid * 16, so that pieces take no address registers each.
 template <class T, int THREADS, int PIECES>
@@ -168,7 +171,7 @@ struct Held {
     }
     // f(values of a piece, number of the piece of thread 0) for pieces in reach of the row
     template <class F>
-    __device__ __forceinline__ void each(const Row<T, THREADS>& x, F f) const {
+    __device__ __forceinline__ void each(const Row<T, THREADS>& x, F f) {
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
             if (i * THREADS < x.pieces) {
@@ -178,7 +181,7 @@ struct Held {
                 __builtin_amdgcn_sched_barrier(0);               // pieces mixed with each other take registers that hold rows
             }
     }
-    __device__ __forceinline__ float max(const Row<T, THREADS>& x) const {
+    __device__ __forceinline__ float max(const Row<T, THREADS>& x) {
         float m = fmaxf(LOWEST, one);
         each(x, [&](const float (&v)[PIECE<T>], int) {
 #pragma unroll
@@ -188,7 +191,7 @@ struct Held {
     }
     // dst[class] = f(value), dst may be the row
     template <class F>
-    __device__ __forceinline__ void map(const Row<T, THREADS>& x, int tid, T* dst, F f) const {
+    __device__ __forceinline__ void map(const Row<T, THREADS>& x, int tid, T* dst, F f) {
         if (at >= 0) dst[at] = (T)f(one);
         const bool alike = (((uintptr_t)dst - (uintptr_t)x.p) & 15u) == 0;
         const uint32_t mine = (uint32_t)tid * 16u;
@@ -204,6 +207,66 @@ struct Held {
         });
     }
 };
+// 16 bytes at any multiple of an element: the hardware takes such addresses.
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ uint4 load_loose(const void* p) {
+    const Loose v = *(const Loose*)p;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store_loose(void* p, const uint4& u) { *(Loose*)p = Loose{u.x, u.y, u.z, u.w}; }
+
+// As Held, but every row is cut from its start on, wherever it begins: class (i THREADS + tid) PIECE + e is element e of piece i in all rows, so that
+// rows of several members can be added in registers.  Classes behind the last whole piece are singles, one a thread.
+template <class T, int THREADS, int PIECES>
+struct Span {
+    uint4 r[PIECES];
+    float one;
+    static __device__ __forceinline__ int single(int len, int tid) { return len / PIECE<T> * PIECE<T> + tid < len ? len / PIECE<T> * PIECE<T> + tid : -1; }
+    __device__ __forceinline__ void load(const T* p, int len, int tid) {
+        const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
+        const int pieces = len / PIECE<T>;
+        const uint32_t mine = (uint32_t)tid * 16u;
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) {
+            const char* const at = (const char*)(p + i * THREADS * PIECE<T>);
+            if ((i + 1) * THREADS <= pieces) r[i] = load_loose(at + mine);
+            else {
+                r[i] = make_uint4(none, none, none, none);
+                if (tid < pieces - i * THREADS) r[i] = load_loose(at + mine);
+            }
+        }
+        one = single(len, tid) >= 0 ? up(p[single(len, tid)]) : NONE;
+    }
+    // f(values of piece i, i)
+    template <class F>
+    __device__ __forceinline__ void each(int len, F f) {
+#pragma unroll
+        for (int i = 0; i < PIECES; i++)
+            if (i * THREADS * PIECE<T> < len) {
+                float v[PIECE<T>];
+                if (sizeof(T) == 2) renew(r[i]);
+                unpack(r[i], v, (const T*)nullptr);
+                f(v, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+};
+// Stores PIECE<T> floats of a row, `to` at any multiple of 4 bytes.
+template <int N>
+__device__ __forceinline__ void store_floats(float* to, const float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+        store_loose(to + e, make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])));
+}
+template <int N>
+__device__ __forceinline__ void load_floats(const float* from, float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        const uint4 u = load_loose(from + e);
+        v[e] = __uint_as_float(u.x); v[e + 1] = __uint_as_float(u.y); v[e + 2] = __uint_as_float(u.z); v[e + 3] = __uint_as_float(u.w);
+    }
+}
+
 template <int N>
 __device__ __forceinline__ float sum_of(const float (&v)[N]) {
     if constexpr (N == 8) return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
