@@ -13,147 +13,230 @@ namespace ens {
 enum { SCORE_SOFTMAX = 0, SCORE_SIGMOID = 1 };
 constexpr int ROUTE_WAVES = 4;
 
-template <class R>
-__device__ __forceinline__ R wave_max_of(R v) {
+// Over the 64 lanes in 64 bits.
+__device__ __forceinline__ double lanes_max(double v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const R w = __shfl_xor(v, o, 64);
-        v = w > v ? w : v;
-    }
+    for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
     return v;
 }
-template <class R>
-__device__ __forceinline__ R wave_sum_of(R v) {
+__device__ __forceinline__ double lanes_sum(double v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
 __device__ __forceinline__ float exp_r(float v) { return expf(v); }
 __device__ __forceinline__ double exp_r(double v) { return exp(v); }
-__device__ __forceinline__ float log1p_r(float v) { return log1pf(v); }
-__device__ __forceinline__ double log1p_r(double v) { return log1p(v); }
 
 // A gate's value; not a member: minus infinity.
+__device__ __forceinline__ float gate_value(float x) { return x > NONE ? fminf(x, -LOWEST) : NONE; }
 template <class R>
-__device__ __forceinline__ R gate_value(float x) { return x > NONE ? (R)fminf(x, -LOWEST) : -(R)__builtin_inf(); }
-template <class R>
-__device__ __forceinline__ R sigmoid_of(R x) { return x >= 0 ? 1 / (1 + exp_r(-x)) : exp_r(x) / (1 + exp_r(x)); }
+__device__ __forceinline__ R sigmoid_of(R x) {
+    const R e = exp_r(x >= 0 ? -x : x);
+    return (x >= 0 ? 1 : e) / (1 + e);
+}
 // Logarithm of the score up to a constant of the row.
-template <class R>
-__device__ __forceinline__ R log_score(int score, R x) {
+__device__ __forceinline__ float log_score(int score, float x) {
     if (score == SCORE_SOFTMAX) return x;
-    return x >= 0 ? -log1p_r(exp_r(-x)) : x - log1p_r(exp_r(x));
+    return fminf(x, 0.f) - log1pf(expf(-fabsf(x)));
 }
 
-// The members of a row, member lane + 64 j in x[j] and its score in s[j].
+// Maximum and sum of e^(x - maximum) over the members of a row.
 template <class R, int PER>
-__device__ __forceinline__ void row_scores(int score, const R (&x)[PER], R (&s)[PER]) {
-    const R none = -(R)__builtin_inf();
-    if (score == SCORE_SIGMOID) {
+__device__ __forceinline__ void softmax_of(const R (&x)[PER], R& m, R& sum) {
+    m = x[0];
 #pragma unroll
-        for (int j = 0; j < PER; j++) s[j] = x[j] > none ? sigmoid_of(x[j]) : 0;
-        return;
-    }
-    R m = none, sum = 0;
+    for (int j = 1; j < PER; j++) m = x[j] > m ? x[j] : m;
+    m = lanes_max(m);
+    sum = 0;
+    if (!(m > NONE)) return;
 #pragma unroll
-    for (int j = 0; j < PER; j++) m = x[j] > m ? x[j] : m;
-    m = wave_max_of(m);
+    for (int j = 0; j < PER; j++) sum += exp_r(x[j] - m);
+    sum = lanes_sum(sum);
+}
+
+// What a row's choice goes by.
+struct Rule {
+    const float* bias;
+    int members, k, score, groups, groups_kept, group_best;
+};
+
+// What members rank by, in c (minus infinity: not there), with a bias or in groups; x as gate_value gives it, member lane + 64 j in x[j].
+template <class R, int PER>
+__device__ __forceinline__ void member_ranks(const Rule& a, int lane, const float (&x)[PER], R (&c)[PER], R& most) {
+    R v[PER], m = 0, sum = 1;
+#pragma unroll
+    for (int j = 0; j < PER; j++) v[j] = x[j];
+    if (a.score == SCORE_SOFTMAX) softmax_of<R, PER>(v, m, sum);
+    most = 0;
 #pragma unroll
     for (int j = 0; j < PER; j++) {
-        s[j] = x[j] > none ? exp_r(x[j] - m) : 0;
-        sum += s[j];
+        const float bias = a.bias && lane + 64 * j < a.members ? a.bias[lane + 64 * j] : 0.f;
+        const R s = a.score == SCORE_SOFTMAX ? exp_r(v[j] - m) / sum : sigmoid_of(v[j]);
+        c[j] = s + (R)bias;
+        if (!(x[j] > NONE) || !(c[j] > (R)NONE)) c[j] = (R)NONE;
+        else most = fmax(most, s + fabs((R)bias));
     }
-    sum = wave_sum_of(sum);
+    most = lanes_max(most);
+}
+
+// Takes members of the groups that do not stay out of c.  `ranks`: PER * 64 values of LDS.  Lanes share a group's members; the least difference
+// between a group that stays and one that does not is returned.
+template <class R, int PER>
+__device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R* ranks) {
+    const R none = (R)NONE;
+    const int size = a.members / a.groups;
+    const int each = 64 >> (32 - __clz(a.groups - 1));           // lanes of a group (two groups at least)
+    const int group = lane / each;
 #pragma unroll
-    for (int j = 0; j < PER; j++) s[j] = sum > 0 ? s[j] / sum : 0;
+    for (int j = 0; j < PER; j++) ranks[lane + 64 * j] = c[j];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    R first = none, second = none;
+    auto take = [&](R v) {
+        second = fmax(second, fmin(first, v));
+        first = fmax(first, v);
+    };
+    if (group < a.groups)
+        for (int i = lane % each; i < size; i += each) take(ranks[group * size + i]);
+    for (int o = 1; o < each; o <<= 1) {
+        const R f = __shfl_xor(first, o, 64), s = __shfl_xor(second, o, 64);
+        take(f);
+        second = fmax(second, s);
+    }
+    const R rank = a.group_best == 2 && second > none ? first + second : first;
+    int better = 0;
+    for (int g = 0; g < a.groups; g++) {
+        const R other = __shfl(rank, g * each, 64);
+        better += other > rank || (other == rank && g < group);
+    }
+    const bool stays = group < a.groups && better < a.groups_kept;
+    const unsigned long long kept = __ballot(stays);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint32_t inverse = ((1u << 20) + size - 1) / size;     // members below 512: e * inverse >> 20 is e / size
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+        const int of = (int)((uint32_t)(lane + 64 * j) * inverse >> 20);
+        if (lane + 64 * j < a.members && !(kept >> (of * each) & 1)) c[j] = none;
+    }
+    if (a.groups_kept == a.groups) return (R)__builtin_inf();
+    const R in = -lanes_max(stays ? -rank : none), out = lanes_max(stays || group >= a.groups ? none : rank);
+    return out > none ? in - out : (R)__builtin_inf();
+}
+
+// The k best of c, the i-th in lane i, -1 behind the last; c is used up.  gap: the least difference between one and the next, the best that is left among
+// them.
+template <class R, int PER>
+__device__ __forceinline__ int best_members(int k, int lane, R (&c)[PER], R& gap) {
+    int mine = -1;
+    R before = (R)__builtin_inf();
+    gap = (R)__builtin_inf();
+    for (int i = 0; i <= k; i++) {
+        R best = c[0];
+#pragma unroll
+        for (int j = 1; j < PER; j++) best = fmax(best, c[j]);
+        best = lanes_max(best);
+        if (!(best > (R)NONE)) break;
+        if (i > 0) gap = fmin(gap, before - best == before - best ? before - best : 0);
+        before = best;
+        if (i == k) break;
+        int at = -1;
+#pragma unroll
+        for (int j = 0; j < PER; j++) {
+            const unsigned long long hit = __ballot(c[j] == best);
+            if (hit && at < 0) {
+                at = 64 * j + __builtin_ctzll(hit);
+                if (lane == (at & 63)) c[j] = (R)NONE;
+            }
+        }
+        if (lane == i) mine = at;
+    }
+    return mine;
+}
+
+// The same in 64 bits, for rows in which 32 do not tell two ranks apart.
+template <class T, int PER>
+__device__ __attribute__((noinline)) int choose_exactly(const Rule a, const T* gates, double* ranks) {
+    const int lane = threadIdx.x & 63;
+    float x[PER];
+    double c[PER], most, gap;
+#pragma unroll
+    for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < a.members ? gate_value(up(gates[lane + 64 * j])) : NONE;
+    member_ranks<double, PER>(a, lane, x, c, most);
+    if (a.groups > 1) drop_groups<double, PER>(a, lane, c, ranks);
+    return best_members<double, PER>(a.k, lane, c, gap);
+}
+
+// Gate values of 16 bits by themselves: value and member in one key.
+template <int PER>
+__device__ __forceinline__ int best_of_keys(int k, int lane, uint32_t (&key)[PER]) {
+    int mine = -1;
+    for (int i = 0; i < k; i++) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int j = 1; j < PER; j++) best = key[j] > best ? key[j] : best;
+        best = lanes_max(best);
+        if (best == 0) break;
+        if (lane == i) mine = 0xFFFF - (int)(best & 0xFFFFu);
+#pragma unroll
+        for (int j = 0; j < PER; j++) key[j] = key[j] == best ? 0 : key[j];
+    }
+    return mine;
 }
 
 template <class T, int PER>
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_kernel(const RouteArgs a) {
-    typedef double R;
     __shared__ int counts[ROUTE_MAX_MEMBERS];
-    __shared__ R ranks[ROUTE_WAVES][PER * 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.members;
-    const R none = -(R)__builtin_inf();
+    __shared__ double ranks[ROUTE_WAVES][PER * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.members;
+    const bool by_value = !a.bias && a.groups == 1;
+    const Rule rule{a.bias, a.members, a.k, a.score, a.groups, a.groups_kept, a.group_best};
     if (a.load) {
         for (int e = threadIdx.x; e < E; e += 64 * ROUTE_WAVES) counts[e] = 0;
         __syncthreads();
     }
     for (int64_t row = (int64_t)blockIdx.x * ROUTE_WAVES + wave; row < a.n; row += (int64_t)gridDim.x * ROUTE_WAVES) {
         const T* const gates = (const T*)a.gates + row * a.ld;
-        R x[PER], s[PER], c[PER];
+        float x[PER];
 #pragma unroll
-        for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value<R>(up(gates[lane + 64 * j])) : none;
-        row_scores<R, PER>(a.score, x, s);
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-            c[j] = none;
-            if (x[j] > none) {
-                c[j] = a.bias ? s[j] + (R)a.bias[lane + 64 * j] : a.groups > 1 ? s[j] : x[j];
-                if (!(c[j] > none)) c[j] = none;
-            }
-        }
-        if (a.groups > 1) {
-            const int size = E / a.groups;
-#pragma unroll
-            for (int j = 0; j < PER; j++) ranks[wave][lane + 64 * j] = c[j];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            R first = none, second = none;
-            if (lane < a.groups)
-                for (int i = 0; i < size; i++) {
-                    const R v = ranks[wave][lane * size + i];
-                    if (v > first) { second = first; first = v; }
-                    else if (v > second) second = v;
-                }
-            const R group = a.group_best == 2 && second > none ? first + second : first;
-            int better = 0;
-            for (int g = 0; g < a.groups; g++) {
-                const R other = __shfl(group, g, 64);
-                better += other > group || (other == group && g < lane);
-            }
-            const unsigned long long kept = __ballot(lane < a.groups && better < a.groups_kept);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value(up(gates[lane + 64 * j])) : NONE;
+        int mine;
+        if (by_value && sizeof(T) == 2) {
+            uint32_t key[PER];
 #pragma unroll
             for (int j = 0; j < PER; j++) {
-                const int e = lane + 64 * j;
-                if (e < E && !(kept >> (e / size) & 1)) c[j] = none;
+                uint32_t b = lane + 64 * j < E ? ((const uint16_t*)gates)[lane + 64 * j] : 0u;
+                b = b == 0x8000u ? 0x8000u : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;      // both zeros are one
+                key[j] = x[j] > NONE ? b << 16 | (uint32_t)(0xFFFF - (lane + 64 * j)) : 0u;
             }
-        }
-        int mine = -1;                                           // lane j keeps the j-th choice
-        for (int i = 0; i < a.k; i++) {
-            R best = none;
-            int at = 0x7FFFFFFF;
-#pragma unroll
-            for (int j = 0; j < PER; j++)
-                if (c[j] > best) { best = c[j]; at = lane + 64 * j; }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                const R b = __shfl_xor(best, o, 64);
-                const int t = __shfl_xor(at, o, 64);
-                if (b > best || (b == best && t < at)) { best = b; at = t; }
-            }
-            if (!(best > none)) break;
-            if (lane == i) mine = at;
-#pragma unroll
-            for (int j = 0; j < PER; j++)
-                if (lane + 64 * j == at) c[j] = none;
-        }
-        R weight = 0;
-        const R own = mine >= 0 ? gate_value<R>(up(gates[mine])) : none;
-        if (a.renormalise) {
-            const R l = mine >= 0 ? log_score(a.score, own) : none, top = wave_max_of(l);
-            const R e = mine >= 0 ? exp_r(l - top) : 0, sum = wave_sum_of(e);
-            weight = mine >= 0 ? e / sum : 0;
+            mine = best_of_keys<PER>(a.k, lane, key);
         } else {
+            float c[PER], most = 0.f, gap, apart = __builtin_inff();
+            if (by_value)
 #pragma unroll
-            for (int j = 0; j < PER; j++) {
-                const R v = __shfl(s[j], mine & 63, 64);
-                if (mine >= 0 && mine >> 6 == j) weight = v;
+                for (int j = 0; j < PER; j++) c[j] = x[j];
+            else {
+                member_ranks<float, PER>(rule, lane, x, c, most);
+                if (a.groups > 1) apart = drop_groups<float, PER>(rule, lane, c, (float*)ranks[wave]);
             }
+            mine = best_members<float, PER>(a.k, lane, c, gap);
+            // a score is off by some 20 units of 2^-24 of itself, a rank by half a unit of its own more, a sum of two by twice that
+            if (!by_value && (!(gap > fmaf(most, 0x1p-18f, 0x1p-120f)) || !(apart > fmaf(most, 0x1p-16f, 0x1p-120f)))) mine = choose_exactly<T, PER>(rule, gates, ranks[wave]);
+        }
+        const float own = mine >= 0 ? gate_value(up(gates[mine])) : NONE;
+        float weight;
+        if (a.renormalise) {
+            const float l = mine >= 0 ? log_score(a.score, own) : NONE, top = lanes_max(l);
+            const float e = mine >= 0 ? expf(l - top) : 0.f, sum = lanes_sum(e);
+            weight = mine >= 0 ? e / sum : 0.f;
+        } else if (a.score == SCORE_SIGMOID) {
+            weight = mine >= 0 ? sigmoid_of(own) : 0.f;
+        } else {
+            float m, sum;
+            softmax_of<float, PER>(x, m, sum);
+            weight = mine >= 0 ? expf(own - m) / sum : 0.f;
         }
         if (lane < a.k) {
             a.chosen[row * a.k + lane] = mine;
-            a.weights[row * a.k + lane] = (float)(weight * (R)a.scale);
+            a.weights[row * a.k + lane] = weight * a.scale;
             if (a.load && mine >= 0) atomicAdd(&counts[mine], 1);
         }
     }
@@ -176,16 +259,16 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_backward_kernel(const 
         int mine = lane < a.k ? a.chosen[row * a.k + lane] : -1;
         if (mine < 0 || mine >= E) mine = -1;
         const float u = mine >= 0 ? a.scale * a.d_weights[row * a.k + lane] : 0.f;
-        const float own = mine >= 0 ? gate_value<float>(up(gates[mine])) : NONE;
+        const float own = mine >= 0 ? gate_value(up(gates[mine])) : NONE;
         if (!(own > NONE)) mine = -1;
         float d[PER], slot = 0.f;                                // of the members; of this lane's choice
 #pragma unroll
         for (int j = 0; j < PER; j++) d[j] = 0.f;
         if (a.renormalise) {
-            const float l = mine >= 0 ? log_score(a.score, own) : NONE, top = wave_max_of(l);
-            const float e = mine >= 0 ? exp_r(l - top) : 0.f, sum = wave_sum_of(e);
+            const float l = mine >= 0 ? log_score(a.score, own) : NONE, top = lanes_max(l);
+            const float e = mine >= 0 ? exp_r(l - top) : 0.f, sum = lanes_sum(e);
             const float r = mine >= 0 ? e / sum : 0.f;
-            const float mean = wave_sum_of(r * u);
+            const float mean = lanes_sum(r * u);
             slot = r * (u - mean);
             if (a.score == SCORE_SIGMOID && mine >= 0) slot *= sigmoid_of(-own);
         } else if (a.score == SCORE_SIGMOID) {
@@ -193,15 +276,18 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_backward_kernel(const 
         } else {
             float x[PER], s[PER], part = 0.f;
 #pragma unroll
-            for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value<float>(up(gates[lane + 64 * j])) : NONE;
-            row_scores<float, PER>(a.score, x, s);
+            for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value(up(gates[lane + 64 * j])) : NONE;
+            float m, sum;
+            softmax_of<float, PER>(x, m, sum);
+#pragma unroll
+            for (int j = 0; j < PER; j++) s[j] = x[j] > NONE ? expf(x[j] - m) / sum : 0.f;
 #pragma unroll
             for (int j = 0; j < PER; j++) {
                 const float v = __shfl(s[j], mine & 63, 64);
                 if (mine >= 0 && mine >> 6 == j) part = v;
             }
             slot = u * part;
-            const float mean = wave_sum_of(slot);
+            const float mean = lanes_sum(slot);
 #pragma unroll
             for (int j = 0; j < PER; j++) d[j] = -s[j] * mean;
         }

@@ -74,26 +74,30 @@ struct Exp {
     __device__ __forceinline__ float to(const Exp& larger) const { return __builtin_amdgcn_exp2f(fmaf(m, larger.c, -larger.b) - rest()); }
 };
 
-// e^d for d <= 0.  The argument is a difference to a maximum, so that its product with log2 e is off by 2^-24 of itself, and the
-// hardware's power of two by one unit more.
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
-
-__device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+// Over the 64 lanes, the result uniform: shifts within rows of 16 lanes, the rows' last lanes to the next row, lane 31 to the upper half.  Lane 63
+// then has them all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t otherwise) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)otherwise, (int)v, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+template <class V, class F>
+__device__ __forceinline__ V lanes_fold(V v, V nothing, F f) {
+    static_assert(sizeof(V) == 4, "a register");
+    auto with = [&](auto ctrl, auto rows) {
+        v = f(v, __builtin_bit_cast(V, moved<decltype(ctrl)::value, decltype(rows)::value>(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, nothing))));
+    };
+    with(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xF>());    // row_shr 1, 2, 4, 8
+    with(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xF>());
+    with(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xF>());
+    with(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xF>());
+    with(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());    // row_bcast 15, 31
+    with(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
-// A running maximum and the sum of e^((x - m) c) that goes with it.
-struct MaxSum { float m, s; };
-__device__ __forceinline__ MaxSum join(const MaxSum a, const MaxSum b, const float c) {
-    const float m = fmaxf(a.m, b.m);
-    return MaxSum{m, a.s * exp_of((a.m - m) * c) + b.s * exp_of((b.m - m) * c)};
-}
+__device__ __forceinline__ float lanes_max(float v) { return lanes_fold(v, NONE, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float lanes_sum(float v) { return lanes_fold(v, 0.f, [](float x, float y) { return x + y; }); }
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return lanes_fold(v, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }); }
+__device__ __forceinline__ int lanes_sum(int v) { return lanes_fold(v, 0, [](int x, int y) { return x + y; }); }
 
 // A row of `len` elements from `p` on, in any alignment to its elements: the elements in front of the first 16-byte boundary and those
 // behind the last whole piece are taken one to a thread, the pieces between them in turn by all.

@@ -32,8 +32,7 @@ __device__ __forceinline__ uint64_t key_of(float v, int c) { return (uint64_t)ke
 
 template <int THREADS>
 __device__ __forceinline__ int group_count(int v, float* box) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    v = lanes_sum(v);
     if constexpr (THREADS > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = __int_as_float(v);
