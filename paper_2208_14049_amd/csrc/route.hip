@@ -11,7 +11,9 @@
 namespace ens {
 
 enum { SCORE_SOFTMAX = 0, SCORE_SIGMOID = 1 };
-constexpr int ROUTE_WAVES = 4;
+// Rows at a time of a workgroup.  A workgroup adds what its rows chose to `load` once for each member, and these additions meet on few addresses: with
+// 4 rows and 2 048 workgroups they took 30 us of 55 (32 768 rows of 256 members).
+template <int PER> constexpr int ROUTE_WAVES = PER == 8 ? 8 : 16;
 
 // Over the 64 lanes in 64 bits.
 __device__ __forceinline__ double lanes_max(double v) {
@@ -24,15 +26,27 @@ __device__ __forceinline__ double lanes_sum(double v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
-__device__ __forceinline__ float exp_r(float v) { return expf(v); }
+__device__ __forceinline__ float exp_r(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }      // for v <= 0, as rows.h says
 __device__ __forceinline__ double exp_r(double v) { return exp(v); }
+__device__ __forceinline__ float over(float x, float y) { return x * __builtin_amdgcn_rcpf(y); }
+__device__ __forceinline__ double over(double x, double y) { return x / y; }
+
+// Member lane * PER + j of a row in v[j], `otherwise` behind the last.
+template <class T, int PER>
+__device__ __forceinline__ void load_members(const T* p, int members, int lane, T otherwise, T (&v)[PER]) {
+    const int first = lane * PER;
+    if (first + PER <= members) load_few(p + first, v);
+    else
+#pragma unroll
+        for (int j = 0; j < PER; j++) v[j] = first + j < members ? p[first + j] : otherwise;
+}
 
 // A gate's value; not a member: minus infinity.
 __device__ __forceinline__ float gate_value(float x) { return x > NONE ? fminf(x, -LOWEST) : NONE; }
 template <class R>
 __device__ __forceinline__ R sigmoid_of(R x) {
     const R e = exp_r(x >= 0 ? -x : x);
-    return (x >= 0 ? 1 : e) / (1 + e);
+    return over(x >= 0 ? 1 : e, 1 + e);
 }
 // Logarithm of the score up to a constant of the row.
 __device__ __forceinline__ float log_score(int score, float x) {
@@ -60,7 +74,7 @@ struct Rule {
     int members, k, score, groups, groups_kept, group_best;
 };
 
-// What members rank by, in c (minus infinity: not there), with a bias or in groups; x as gate_value gives it, member lane + 64 j in x[j].
+// What members rank by, in c (minus infinity: not there), with a bias or in groups; x as gate_value gives it, member lane * PER + j in x[j].
 template <class R, int PER>
 __device__ __forceinline__ void member_ranks(const Rule& a, int lane, const float (&x)[PER], R (&c)[PER], R& most) {
     R v[PER], m = 0, sum = 1;
@@ -68,13 +82,17 @@ __device__ __forceinline__ void member_ranks(const Rule& a, int lane, const floa
     for (int j = 0; j < PER; j++) v[j] = x[j];
     if (a.score == SCORE_SOFTMAX) softmax_of<R, PER>(v, m, sum);
     most = 0;
+    float bias[PER];
+#pragma unroll
+    for (int j = 0; j < PER; j++) bias[j] = 0.f;
+    if (a.bias) load_members(a.bias, a.members, lane, 0.f, bias);
+    const R inverse = over((R)1, sum);
 #pragma unroll
     for (int j = 0; j < PER; j++) {
-        const float bias = a.bias && lane + 64 * j < a.members ? a.bias[lane + 64 * j] : 0.f;
-        const R s = a.score == SCORE_SOFTMAX ? exp_r(v[j] - m) / sum : sigmoid_of(v[j]);
-        c[j] = s + (R)bias;
+        const R s = a.score == SCORE_SOFTMAX ? exp_r(v[j] - m) * inverse : sigmoid_of(v[j]);
+        c[j] = s + (R)bias[j];
         if (!(x[j] > NONE) || !(c[j] > (R)NONE)) c[j] = (R)NONE;
-        else most = fmax(most, s + fabs((R)bias));
+        else most = fmax(most, s + fabs((R)bias[j]));
     }
     most = lanes_max(most);
 }
@@ -88,7 +106,7 @@ __device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R
     const int each = 64 >> (32 - __clz(a.groups - 1));           // lanes of a group (two groups at least)
     const int group = lane / each;
 #pragma unroll
-    for (int j = 0; j < PER; j++) ranks[lane + 64 * j] = c[j];
+    for (int j = 0; j < PER; j++) ranks[lane * PER + j] = c[j];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     R first = none, second = none;
     auto take = [&](R v) {
@@ -114,8 +132,8 @@ __device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R
     const uint32_t inverse = ((1u << 20) + size - 1) / size;     // members below 512: e * inverse >> 20 is e / size
 #pragma unroll
     for (int j = 0; j < PER; j++) {
-        const int of = (int)((uint32_t)(lane + 64 * j) * inverse >> 20);
-        if (lane + 64 * j < a.members && !(kept >> (of * each) & 1)) c[j] = none;
+        const int of = (int)((uint32_t)(lane * PER + j) * inverse >> 20);
+        if (lane * PER + j < a.members && !(kept >> (of * each) & 1)) c[j] = none;
     }
     if (a.groups_kept == a.groups) return (R)__builtin_inf();
     const R in = -lanes_max(stays ? -rank : none), out = lanes_max(stays || group >= a.groups ? none : rank);
@@ -138,15 +156,13 @@ __device__ __forceinline__ int best_members(int k, int lane, R (&c)[PER], R& gap
         if (i > 0) gap = fmin(gap, before - best == before - best ? before - best : 0);
         before = best;
         if (i == k) break;
-        int at = -1;
+        // the lowest member: the first lane that has the value, the first of its members
+        int own = -1;
 #pragma unroll
-        for (int j = 0; j < PER; j++) {
-            const unsigned long long hit = __ballot(c[j] == best);
-            if (hit && at < 0) {
-                at = 64 * j + __builtin_ctzll(hit);
-                if (lane == (at & 63)) c[j] = (R)NONE;
-            }
-        }
+        for (int j = PER - 1; j >= 0; j--) own = c[j] == best ? j : own;
+        const int owner = __builtin_ctzll(__ballot(own >= 0)), at = owner * PER + __builtin_amdgcn_readlane(own, owner);
+#pragma unroll
+        for (int j = 0; j < PER; j++) c[j] = lane == owner && own == j ? (R)NONE : c[j];
         if (lane == i) mine = at;
     }
     return mine;
@@ -156,14 +172,20 @@ __device__ __forceinline__ int best_members(int k, int lane, R (&c)[PER], R& gap
 template <class T, int PER>
 __device__ __attribute__((noinline)) int choose_exactly(const Rule a, const T* gates, double* ranks) {
     const int lane = threadIdx.x & 63;
+    T raw[PER];
     float x[PER];
     double c[PER], most, gap;
+    load_members(gates, a.members, lane, (T)NONE, raw);
 #pragma unroll
-    for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < a.members ? gate_value(up(gates[lane + 64 * j])) : NONE;
+    for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));
     member_ranks<double, PER>(a, lane, x, c, most);
     if (a.groups > 1) drop_groups<double, PER>(a, lane, c, ranks);
     return best_members<double, PER>(a.k, lane, c, gap);
 }
+
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t bits_of(__bf16 v) { return __builtin_bit_cast(uint16_t, v); }
+__device__ __forceinline__ uint32_t bits_of(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
 
 // Gate values of 16 bits by themselves: value and member in one key.
 template <int PER>
@@ -183,29 +205,32 @@ __device__ __forceinline__ int best_of_keys(int k, int lane, uint32_t (&key)[PER
 }
 
 template <class T, int PER>
-__global__ __launch_bounds__(64 * ROUTE_WAVES) void route_kernel(const RouteArgs a) {
-    __shared__ int counts[ROUTE_MAX_MEMBERS];
-    __shared__ double ranks[ROUTE_WAVES][PER * 64];
+__global__ __launch_bounds__(64 * ROUTE_WAVES<PER>) void route_kernel(const RouteArgs a) {
+    constexpr int WAVES = ROUTE_WAVES<PER>;
+    __shared__ int counts[PER * 64];
+    __shared__ double ranks[WAVES][PER * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.members;
     const bool by_value = !a.bias && a.groups == 1;
     const Rule rule{a.bias, a.members, a.k, a.score, a.groups, a.groups_kept, a.group_best};
     if (a.load) {
-        for (int e = threadIdx.x; e < E; e += 64 * ROUTE_WAVES) counts[e] = 0;
+        for (int e = threadIdx.x; e < E; e += 64 * WAVES) counts[e] = 0;
         __syncthreads();
     }
-    for (int64_t row = (int64_t)blockIdx.x * ROUTE_WAVES + wave; row < a.n; row += (int64_t)gridDim.x * ROUTE_WAVES) {
+    for (int64_t row = (int64_t)blockIdx.x * WAVES + wave; row < a.n; row += (int64_t)gridDim.x * WAVES) {
         const T* const gates = (const T*)a.gates + row * a.ld;
+        T raw[PER];
         float x[PER];
+        load_members(gates, E, lane, (T)NONE, raw);
 #pragma unroll
-        for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value(up(gates[lane + 64 * j])) : NONE;
+        for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));
         int mine;
         if (by_value && sizeof(T) == 2) {
             uint32_t key[PER];
 #pragma unroll
             for (int j = 0; j < PER; j++) {
-                uint32_t b = lane + 64 * j < E ? ((const uint16_t*)gates)[lane + 64 * j] : 0u;
+                uint32_t b = bits_of(raw[j]);
                 b = b == 0x8000u ? 0x8000u : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;      // both zeros are one
-                key[j] = x[j] > NONE ? b << 16 | (uint32_t)(0xFFFF - (lane + 64 * j)) : 0u;
+                key[j] = x[j] > NONE ? b << 16 | (uint32_t)(0xFFFF - (lane * PER + j)) : 0u;
             }
             mine = best_of_keys<PER>(a.k, lane, key);
         } else {
@@ -242,7 +267,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_kernel(const RouteArgs
     }
     if (a.load) {
         __syncthreads();
-        for (int e = threadIdx.x; e < E; e += 64 * ROUTE_WAVES)
+        for (int e = threadIdx.x; e < E; e += 64 * WAVES)
             if (counts[e]) atomicAdd(&a.load[e], counts[e]);
     }
 }
@@ -251,57 +276,76 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_kernel(const RouteArgs
 // sigmoid: times 1 - s_j.  As they are: softmax dL/dx_e = s_e (u_e - sum u_j s_j), sigmoid dL/dx_j = u_j s_j (1 - s_j).
 // The choice itself has no derivative.
 template <class T, int PER>
-__global__ __launch_bounds__(64 * ROUTE_WAVES) void route_backward_kernel(const RouteArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.members;
-    for (int64_t row = (int64_t)blockIdx.x * ROUTE_WAVES + wave; row < a.n; row += (int64_t)gridDim.x * ROUTE_WAVES) {
+__global__ __launch_bounds__(64 * ROUTE_WAVES<PER>) void route_backward_kernel(const RouteArgs a) {
+    constexpr int WAVES = ROUTE_WAVES<PER>;
+    __shared__ float parts[WAVES][PER * 64];                     // of the row's members, zeros between rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.members;
+    float* const part = parts[wave];
+#pragma unroll
+    for (int j = 0; j < PER; j++) part[lane * PER + j] = 0.f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int64_t row = (int64_t)blockIdx.x * WAVES + wave; row < a.n; row += (int64_t)gridDim.x * WAVES) {
         const T* const gates = (const T*)a.gates + row * a.ld;
-        T* const out = (T*)a.d_gates + row * a.ld_d;
         int mine = lane < a.k ? a.chosen[row * a.k + lane] : -1;
         if (mine < 0 || mine >= E) mine = -1;
         const float u = mine >= 0 ? a.scale * a.d_weights[row * a.k + lane] : 0.f;
         const float own = mine >= 0 ? gate_value(up(gates[mine])) : NONE;
         if (!(own > NONE)) mine = -1;
-        float d[PER], slot = 0.f;                                // of the members; of this lane's choice
-#pragma unroll
-        for (int j = 0; j < PER; j++) d[j] = 0.f;
+        const bool dense = !a.renormalise && a.score == SCORE_SOFTMAX;
+        float slot = 0.f, mean = 0.f, m = 0.f, sum = 1.f;
+        T raw[PER];
         if (a.renormalise) {
             const float l = mine >= 0 ? log_score(a.score, own) : NONE, top = lanes_max(l);
-            const float e = mine >= 0 ? exp_r(l - top) : 0.f, sum = lanes_sum(e);
-            const float r = mine >= 0 ? e / sum : 0.f;
-            const float mean = lanes_sum(r * u);
-            slot = r * (u - mean);
+            const float e = mine >= 0 ? expf(l - top) : 0.f, total = lanes_sum(e);
+            const float r = mine >= 0 ? e / total : 0.f;
+            slot = r * (u - lanes_sum(r * u));
             if (a.score == SCORE_SIGMOID && mine >= 0) slot *= sigmoid_of(-own);
         } else if (a.score == SCORE_SIGMOID) {
             if (mine >= 0) slot = u * sigmoid_of(own) * sigmoid_of(-own);
         } else {
-            float x[PER], s[PER], part = 0.f;
+            float x[PER];
+            load_members(gates, E, lane, (T)NONE, raw);
 #pragma unroll
-            for (int j = 0; j < PER; j++) x[j] = lane + 64 * j < E ? gate_value(up(gates[lane + 64 * j])) : NONE;
-            float m, sum;
+            for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));
             softmax_of<float, PER>(x, m, sum);
+            if (mine >= 0) slot = u * (expf(own - m) / sum);
+            mean = lanes_sum(slot);
+        }
+        // to the members through LDS; a member that was chosen twice gets both, in order
+        if (mine >= 0) part[mine] = __int_as_float(lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const bool twice = mine >= 0 && __float_as_int(part[mine]) != lane;
+        if (__ballot(twice) == 0) {
+            if (mine >= 0) part[mine] = slot;
+        } else {
+            if (mine >= 0) part[mine] = 0.f;
+            for (int i = 0; i < a.k; i++) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                if (lane == i && mine >= 0) part[mine] += slot;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float d[PER];
+        T out[PER];
 #pragma unroll
-            for (int j = 0; j < PER; j++) s[j] = x[j] > NONE ? expf(x[j] - m) / sum : 0.f;
+        for (int j = 0; j < PER; j++) d[j] = part[lane * PER + j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (mine >= 0) part[mine] = 0.f;
+        if (dense)
 #pragma unroll
             for (int j = 0; j < PER; j++) {
-                const float v = __shfl(s[j], mine & 63, 64);
-                if (mine >= 0 && mine >> 6 == j) part = v;
+                const float x = gate_value(up(raw[j]));
+                if (x > NONE) d[j] -= expf(x - m) / sum * mean;
             }
-            slot = u * part;
-            const float mean = lanes_sum(slot);
 #pragma unroll
-            for (int j = 0; j < PER; j++) d[j] = -s[j] * mean;
-        }
-        for (int i = 0; i < a.k; i++) {                          // a member that was chosen twice gets both
-            const int e = __builtin_amdgcn_readlane(mine, i);
-            const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(slot), i));
-            if (e < 0) continue;
+        for (int j = 0; j < PER; j++) out[j] = (T)d[j];
+        T* const to = (T*)a.d_gates + row * a.ld_d + lane * PER;
+        if ((lane + 1) * PER <= E) store_few(to, out);
+        else
 #pragma unroll
             for (int j = 0; j < PER; j++)
-                if (lane + 64 * j == e) d[j] += v;
-        }
-#pragma unroll
-        for (int j = 0; j < PER; j++)
-            if (lane + 64 * j < E) out[lane + 64 * j] = (T)d[j];
+                if (lane * PER + j < E) to[j] = out[j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -313,12 +357,15 @@ static hipError_t by_members(int members, F f) {
     return f(std::integral_constant<int, 8>());
 }
 
-static unsigned route_blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + ROUTE_WAVES - 1) / ROUTE_WAVES, 2048); }
+// Two workgroups of a compute unit's 32 wavefronts.
+template <int PER>
+static unsigned route_blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + ROUTE_WAVES<PER> - 1) / ROUTE_WAVES<PER>, 8192 / ROUTE_WAVES<PER>); }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     return by_type(a.dtype, [&](auto t) {
         return by_members(a.members, [&](auto per) {
-            hipLaunchKernelGGL((route_kernel<decltype(t), decltype(per)::value>), dim3(route_blocks(a.n)), dim3(64 * ROUTE_WAVES), 0, s, a);
+            constexpr int PER = decltype(per)::value;
+            hipLaunchKernelGGL((route_kernel<decltype(t), PER>), dim3(route_blocks<PER>(a.n)), dim3(64 * ROUTE_WAVES<PER>), 0, s, a);
             return hipGetLastError();
         });
     });
@@ -327,7 +374,8 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s) {
     return by_type(a.dtype, [&](auto t) {
         return by_members(a.members, [&](auto per) {
-            hipLaunchKernelGGL((route_backward_kernel<decltype(t), decltype(per)::value>), dim3(route_blocks(a.n)), dim3(64 * ROUTE_WAVES), 0, s, a);
+            constexpr int PER = decltype(per)::value;
+            hipLaunchKernelGGL((route_backward_kernel<decltype(t), PER>), dim3(route_blocks<PER>(a.n)), dim3(64 * ROUTE_WAVES<PER>), 0, s, a);
             return hipGetLastError();
         });
     });

@@ -219,6 +219,22 @@ __device__ __forceinline__ uint4 load_loose(const void* p) {
 }
 __device__ __forceinline__ void store_loose(void* p, const uint4& u) { *(Loose*)p = Loose{u.x, u.y, u.z, u.w}; }
 
+// N elements (2 to 32 bytes of them) at any multiple of an element.
+template <class T, int N>
+__device__ __forceinline__ void load_few(const T* p, T (&v)[N]) {
+    struct __attribute__((packed, aligned(2))) Few { T v[N]; };
+    const Few f = *(const Few*)p;
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = f.v[i];
+}
+template <class T, int N>
+__device__ __forceinline__ void store_few(T* p, const T (&v)[N]) {
+    struct __attribute__((packed, aligned(2))) Few { T v[N]; } f;
+#pragma unroll
+    for (int i = 0; i < N; i++) f.v[i] = v[i];
+    *(Few*)p = f;
+}
+
 // As Held, but every row is cut from its start on, wherever it begins: class (i THREADS + tid) PIECE + e is element e of piece i in all rows, so that
 // rows of several members can be added in registers.  Classes behind the last whole piece are singles, one a thread.
 template <class T, int THREADS, int PIECES>
