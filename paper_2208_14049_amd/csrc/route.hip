@@ -26,6 +26,12 @@ __device__ __forceinline__ double lanes_sum(double v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
+__device__ __forceinline__ float of_lane(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+__device__ __forceinline__ double of_lane(double v, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)b, lane), high = __builtin_amdgcn_readlane((uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
 __device__ __forceinline__ float exp_r(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }      // for v <= 0, as rows.h says
 __device__ __forceinline__ double exp_r(double v) { return exp(v); }
 __device__ __forceinline__ float over(float x, float y) { return x * __builtin_amdgcn_rcpf(y); }
@@ -123,7 +129,7 @@ __device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R
     const R rank = a.group_best == 2 && second > none ? first + second : first;
     int better = 0;
     for (int g = 0; g < a.groups; g++) {
-        const R other = __shfl(rank, g * each, 64);
+        const R other = of_lane(rank, g * each);
         better += other > rank || (other == rank && g < group);
     }
     const bool stays = group < a.groups && better < a.groups_kept;
@@ -140,23 +146,65 @@ __device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R
     return out > none ? in - out : (R)__builtin_inf();
 }
 
-// The k best of c, the i-th in lane i, -1 behind the last; c is used up.  gap: the least difference between one and the next, the best that is left among
-// them.
+// Puts a lane's ranks in falling order, the members' numbers in the lane (first the lower one, among equal ranks in no order) with them.
 template <class R, int PER>
-__device__ __forceinline__ int best_members(int k, int lane, R (&c)[PER], R& gap) {
-    int mine = -1;
-    R before = (R)__builtin_inf();
-    gap = (R)__builtin_inf();
+__device__ __forceinline__ void sort_lane(R (&c)[PER], int (&number)[PER]) {
+#pragma unroll
+    for (int j = 0; j < PER; j++) number[j] = j;
+#pragma unroll
+    for (int size = 2; size <= PER; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                const int o = i ^ step;
+                if (o < i) continue;
+                const bool falling = (i & size) == 0 || size == PER;
+                const bool swap = falling ? c[i] < c[o] : c[o] < c[i];
+                const R ci = swap ? c[o] : c[i], co = swap ? c[i] : c[o];
+                const int ni = swap ? number[o] : number[i], no = swap ? number[i] : number[o];
+                c[i] = ci; c[o] = co; number[i] = ni; number[o] = no;
+            }
+}
+
+// The k best of c, the i-th in lane i, -1 behind the last; c is used up.  gap: the least difference between one and the next, the best that is left among
+// them.  Members of equal rank come in no order, with a gap of 0.
+template <int PER>
+__device__ __forceinline__ int best_members(int k, int lane, float (&c)[PER], float& gap) {
+    int mine = -1, number[PER];
+    sort_lane<float, PER>(c, number);
+    float before = __builtin_inff();
+    gap = __builtin_inff();
     for (int i = 0; i <= k; i++) {
+        const float best = lanes_max(c[0]);
+        if (!(best > NONE)) break;
+        if (i > 0) gap = fminf(gap, before == best ? 0.f : before - best);
+        before = best;
+        if (i == k) break;
+        const int owner = __builtin_ctzll(__ballot(c[0] == best)), at = owner * PER + __builtin_amdgcn_readlane(number[0], owner);
+        if (lane == i) mine = at;
+        if (lane == owner) {
+#pragma unroll
+            for (int j = 0; j + 1 < PER; j++) {
+                c[j] = c[j + 1];
+                number[j] = number[j + 1];
+            }
+            c[PER - 1] = NONE;
+        }
+    }
+    return mine;
+}
+
+// The same with the lowest member first among equal ranks.
+template <class R, int PER>
+__device__ __forceinline__ int best_in_order(int k, int lane, R (&c)[PER]) {
+    int mine = -1;
+    for (int i = 0; i < k; i++) {
         R best = c[0];
 #pragma unroll
         for (int j = 1; j < PER; j++) best = fmax(best, c[j]);
         best = lanes_max(best);
         if (!(best > (R)NONE)) break;
-        if (i > 0) gap = fmin(gap, before - best == before - best ? before - best : 0);
-        before = best;
-        if (i == k) break;
-        // the lowest member: the first lane that has the value, the first of its members
         int own = -1;
 #pragma unroll
         for (int j = PER - 1; j >= 0; j--) own = c[j] == best ? j : own;
@@ -174,77 +222,96 @@ __device__ __attribute__((noinline)) int choose_exactly(const Rule a, const T* g
     const int lane = threadIdx.x & 63;
     T raw[PER];
     float x[PER];
-    double c[PER], most, gap;
+    double c[PER], most;
     load_members(gates, a.members, lane, (T)NONE, raw);
 #pragma unroll
     for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));
     member_ranks<double, PER>(a, lane, x, c, most);
     if (a.groups > 1) drop_groups<double, PER>(a, lane, c, ranks);
-    return best_members<double, PER>(a.k, lane, c, gap);
+    return best_in_order<double, PER>(a.k, lane, c);
 }
 
 __device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
 __device__ __forceinline__ uint32_t bits_of(__bf16 v) { return __builtin_bit_cast(uint16_t, v); }
 __device__ __forceinline__ uint32_t bits_of(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
 
-// Gate values of 16 bits by themselves: value and member in one key.
+// Gate values of 16 bits by themselves: value and member in one key, no two alike and 0 for what is not there.
 template <int PER>
 __device__ __forceinline__ int best_of_keys(int k, int lane, uint32_t (&key)[PER]) {
     int mine = -1;
-    for (int i = 0; i < k; i++) {
-        uint32_t best = key[0];
 #pragma unroll
-        for (int j = 1; j < PER; j++) best = key[j] > best ? key[j] : best;
-        best = lanes_max(best);
+    for (int size = 2; size <= PER; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                const int o = i ^ step;
+                if (o < i) continue;
+                const uint32_t low = min(key[i], key[o]), high = max(key[i], key[o]);
+                const bool falling = (i & size) == 0 || size == PER;
+                key[i] = falling ? high : low;
+                key[o] = falling ? low : high;
+            }
+    for (int i = 0; i < k; i++) {
+        const uint32_t best = lanes_max(key[0]);
         if (best == 0) break;
         if (lane == i) mine = 0xFFFF - (int)(best & 0xFFFFu);
+        const uint32_t taken = key[0] == best ? ~0u : 0u;
 #pragma unroll
-        for (int j = 0; j < PER; j++) key[j] = key[j] == best ? 0 : key[j];
+        for (int j = 0; j + 1 < PER; j++) key[j] = (key[j + 1] & taken) | (key[j] & ~taken);
+        key[PER - 1] &= ~taken;
     }
     return mine;
 }
 
-template <class T, int PER>
-__global__ __launch_bounds__(64 * ROUTE_WAVES<PER>) void route_kernel(const RouteArgs a) {
+// BY_VALUE: members rank by the gate's values themselves (no bias, no groups).
+template <class T, int PER, bool BY_VALUE>
+__global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route_kernel(const RouteArgs a) {
     constexpr int WAVES = ROUTE_WAVES<PER>;
     __shared__ int counts[PER * 64];
-    __shared__ double ranks[WAVES][PER * 64];
+    __shared__ double ranks[BY_VALUE ? 1 : WAVES][PER * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.members;
-    const bool by_value = !a.bias && a.groups == 1;
     const Rule rule{a.bias, a.members, a.k, a.score, a.groups, a.groups_kept, a.group_best};
     if (a.load) {
         for (int e = threadIdx.x; e < E; e += 64 * WAVES) counts[e] = 0;
         __syncthreads();
     }
-    for (int64_t row = (int64_t)blockIdx.x * WAVES + wave; row < a.n; row += (int64_t)gridDim.x * WAVES) {
+    const int64_t first = (int64_t)blockIdx.x * WAVES + wave, step = (int64_t)gridDim.x * WAVES;
+    T next[PER];
+    if (first < a.n) load_members((const T*)a.gates + first * a.ld, E, lane, (T)NONE, next);
+    for (int64_t row = first; row < a.n; row += step) {
         const T* const gates = (const T*)a.gates + row * a.ld;
         T raw[PER];
         float x[PER];
-        load_members(gates, E, lane, (T)NONE, raw);
 #pragma unroll
-        for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));
+        for (int j = 0; j < PER; j++) {
+            raw[j] = next[j];
+            x[j] = gate_value(up(raw[j]));
+        }
+        if (row + step < a.n) load_members(gates + step * a.ld, E, lane, (T)NONE, next);
         int mine;
-        if (by_value && sizeof(T) == 2) {
+        if constexpr (BY_VALUE && sizeof(T) == 2) {
             uint32_t key[PER];
 #pragma unroll
             for (int j = 0; j < PER; j++) {
-                uint32_t b = bits_of(raw[j]);
-                b = b == 0x8000u ? 0x8000u : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;      // both zeros are one
-                key[j] = x[j] > NONE ? b << 16 | (uint32_t)(0xFFFF - (lane * PER + j)) : 0u;
+                uint32_t b = bits_of(raw[j]) << 16;
+                b = b == 0x80000000u ? 0u : b;                   // both zeros are one
+                b ^= (uint32_t)((int32_t)b >> 31) | 0x80000000u;
+                key[j] = x[j] > NONE ? (b & 0xFFFF0000u) | (uint32_t)(0xFFFF - (lane * PER + j)) : 0u;
             }
             mine = best_of_keys<PER>(a.k, lane, key);
-        } else {
-            float c[PER], most = 0.f, gap, apart = __builtin_inff();
-            if (by_value)
+        } else if constexpr (BY_VALUE) {
+            float c[PER];
 #pragma unroll
-                for (int j = 0; j < PER; j++) c[j] = x[j];
-            else {
-                member_ranks<float, PER>(rule, lane, x, c, most);
-                if (a.groups > 1) apart = drop_groups<float, PER>(rule, lane, c, (float*)ranks[wave]);
-            }
-            mine = best_members<float, PER>(a.k, lane, c, gap);
+            for (int j = 0; j < PER; j++) c[j] = x[j];
+            mine = best_in_order<float, PER>(a.k, lane, c);
+        } else {
+            float c[PER], most, gap, apart = __builtin_inff();
+            member_ranks<float, PER>(rule, lane, x, c, most);
+            if (a.groups > 1) apart = drop_groups<float, PER>(rule, lane, c, (float*)ranks[wave]);
+            mine = best_members<PER>(a.k, lane, c, gap);
             // a score is off by some 20 units of 2^-24 of itself, a rank by half a unit of its own more, a sum of two by twice that
-            if (!by_value && (!(gap > fmaf(most, 0x1p-18f, 0x1p-120f)) || !(apart > fmaf(most, 0x1p-16f, 0x1p-120f)))) mine = choose_exactly<T, PER>(rule, gates, ranks[wave]);
+            if (!(gap > fmaf(most, 0x1p-18f, 0x1p-120f) && apart > fmaf(most, 0x1p-16f, 0x1p-120f))) mine = choose_exactly<T, PER>(rule, gates, ranks[wave]);
         }
         const float own = mine >= 0 ? gate_value(up(gates[mine])) : NONE;
         float weight;
@@ -365,7 +432,9 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     return by_type(a.dtype, [&](auto t) {
         return by_members(a.members, [&](auto per) {
             constexpr int PER = decltype(per)::value;
-            hipLaunchKernelGGL((route_kernel<decltype(t), PER>), dim3(route_blocks<PER>(a.n)), dim3(64 * ROUTE_WAVES<PER>), 0, s, a);
+            const dim3 grid(route_blocks<PER>(a.n)), group(64 * ROUTE_WAVES<PER>);
+            if (!a.bias && a.groups == 1) hipLaunchKernelGGL((route_kernel<decltype(t), PER, true>), grid, group, 0, s, a);
+            else hipLaunchKernelGGL((route_kernel<decltype(t), PER, false>), grid, group, 0, s, a);
             return hipGetLastError();
         });
     });
