@@ -146,11 +146,17 @@ __device__ __forceinline__ R drop_groups(const Rule& a, int lane, R (&c)[PER], R
     return out > none ? in - out : (R)__builtin_inf();
 }
 
-// Puts a lane's ranks in falling order, the members' numbers in the lane (first the lower one, among equal ranks in no order) with them.
-template <class R, int PER>
-__device__ __forceinline__ void sort_lane(R (&c)[PER], int (&number)[PER]) {
+// The k best of c, the i-th in lane i, -1 behind the last.  gap: the least difference between one and the next, the best that is left among
+// them.  Members of equal rank come in no order, with a gap of 0.
+template <int PER>
+__device__ __forceinline__ int best_members(int k, int lane, const float (&c)[PER], float& gap) {
+    // the lane's ranks in falling order, as whole numbers (0: not there), and the members' numbers in the lane with them
+    uint32_t key[PER], number[PER];
 #pragma unroll
-    for (int j = 0; j < PER; j++) number[j] = j;
+    for (int j = 0; j < PER; j++) {
+        key[j] = c[j] > NONE ? ordered(c[j]) : 0u;
+        number[j] = j;
+    }
 #pragma unroll
     for (int size = 2; size <= PER; size *= 2)
 #pragma unroll
@@ -160,37 +166,29 @@ __device__ __forceinline__ void sort_lane(R (&c)[PER], int (&number)[PER]) {
                 const int o = i ^ step;
                 if (o < i) continue;
                 const bool falling = (i & size) == 0 || size == PER;
-                const bool swap = falling ? c[i] < c[o] : c[o] < c[i];
-                const R ci = swap ? c[o] : c[i], co = swap ? c[i] : c[o];
-                const int ni = swap ? number[o] : number[i], no = swap ? number[i] : number[o];
-                c[i] = ci; c[o] = co; number[i] = ni; number[o] = no;
+                const uint32_t swap = (falling ? key[i] < key[o] : key[o] < key[i]) ? ~0u : 0u;
+                const uint32_t keys = (key[i] ^ key[o]) & swap, numbers = (number[i] ^ number[o]) & swap;
+                key[i] ^= keys; key[o] ^= keys; number[i] ^= numbers; number[o] ^= numbers;
             }
-}
-
-// The k best of c, the i-th in lane i, -1 behind the last; c is used up.  gap: the least difference between one and the next, the best that is left among
-// them.  Members of equal rank come in no order, with a gap of 0.
-template <int PER>
-__device__ __forceinline__ int best_members(int k, int lane, float (&c)[PER], float& gap) {
-    int mine = -1, number[PER];
-    sort_lane<float, PER>(c, number);
+    int mine = -1;
     float before = __builtin_inff();
     gap = __builtin_inff();
     for (int i = 0; i <= k; i++) {
-        const float best = lanes_max(c[0]);
-        if (!(best > NONE)) break;
+        const uint32_t most = lanes_max(key[0]);
+        if (most == 0) break;
+        const float best = unordered(most);
         if (i > 0) gap = fminf(gap, before == best ? 0.f : before - best);
         before = best;
         if (i == k) break;
-        const int owner = __builtin_ctzll(__ballot(c[0] == best)), at = owner * PER + __builtin_amdgcn_readlane(number[0], owner);
+        const int owner = __builtin_ctzll(__ballot(key[0] == most)), at = owner * PER + __builtin_amdgcn_readlane(number[0], owner);
         if (lane == i) mine = at;
-        if (lane == owner) {
+        const uint32_t taken = lane == owner ? ~0u : 0u;
 #pragma unroll
-            for (int j = 0; j + 1 < PER; j++) {
-                c[j] = c[j + 1];
-                number[j] = number[j + 1];
-            }
-            c[PER - 1] = NONE;
+        for (int j = 0; j + 1 < PER; j++) {
+            key[j] = (key[j + 1] & taken) | (key[j] & ~taken);
+            number[j] = (number[j + 1] & taken) | (number[j] & ~taken);
         }
+        key[PER - 1] &= ~taken;
     }
     return mine;
 }

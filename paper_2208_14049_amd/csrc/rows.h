@@ -74,6 +74,13 @@ struct Exp {
     __device__ __forceinline__ float to(const Exp& larger) const { return __builtin_amdgcn_exp2f(fmaf(m, larger.c, -larger.b) - rest()); }
 };
 
+// A whole number in the order of a float that is no NaN, and back.
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t key) { return __uint_as_float(key ^ ((uint32_t)((int32_t)~key >> 31) | 0x80000000u)); }
+
 // Over the 64 lanes, the result uniform: shifts within rows of 16 lanes, the rows' last lanes to the next row, lane 31 to the upper half.  Lane 63
 // then has them all.
 template <int CTRL, int ROWS>
@@ -94,9 +101,10 @@ __device__ __forceinline__ V lanes_fold(V v, V nothing, F f) {
     with(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());
     return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
-__device__ __forceinline__ float lanes_max(float v) { return lanes_fold(v, NONE, [](float x, float y) { return fmaxf(x, y); }); }
-__device__ __forceinline__ float lanes_sum(float v) { return lanes_fold(v, 0.f, [](float x, float y) { return x + y; }); }
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return lanes_fold(v, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }); }
+// (of no NaN: as whole numbers, whose maximum is one instruction a shift where that of floats is four)
+__device__ __forceinline__ float lanes_max(float v) { return unordered(lanes_max(ordered(v))); }
+__device__ __forceinline__ float lanes_sum(float v) { return lanes_fold(v, 0.f, [](float x, float y) { return x + y; }); }
 __device__ __forceinline__ int lanes_sum(int v) { return lanes_fold(v, 0, [](int x, int y) { return x + y; }); }
 
 // A row of `len` elements from `p` on, in any alignment to its elements: the elements in front of the first 16-byte boundary and those

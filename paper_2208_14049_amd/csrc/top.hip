@@ -19,14 +19,8 @@ constexpr int TOP_ROOM = 1024, TOP_WAVE_ROOM = 256;     // candidates in LDS
 constexpr int TOP_WAVE_K = 32;                          // for which the 64 lanes of a wavefront are groups enough
 constexpr int JOIN_THREADS = 256, JOIN_KEYS = 2048;     // keys of a row's parts: 8 a thread, so that 128 threads' keys have room
 
-__device__ __forceinline__ uint32_t key_of(float v) {
-    const uint32_t b = __float_as_uint(v + 0.f);                 // both zeros are one
-    return v != v ? 0u : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float value_of(uint32_t key) {
-    if (key == 0u) return __uint_as_float(0x7FC00000u);
-    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-}
+__device__ __forceinline__ uint32_t key_of(float v) { return v != v ? 0u : ordered(v + 0.f); }      // both zeros are one
+__device__ __forceinline__ float value_of(uint32_t key) { return key == 0u ? __uint_as_float(0x7FC00000u) : unordered(key); }
 // Larger value first, then lower class; no key is 0.
 __device__ __forceinline__ uint64_t key_of(float v, int c) { return (uint64_t)key_of(v) << 32 | (0xFFFFFFFFu - (uint32_t)c); }
 
