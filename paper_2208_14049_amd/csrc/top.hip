@@ -6,7 +6,7 @@
 // the maxima, a second one at the pieces that hold something, and a third for the sum of a softmax.
 // Where too many values are no smaller than t (equal ones, most of the row masked, the large ones in few lanes), or too few (NaN), the bound is found
 // by halving, over the row in memory.
-// Few or long rows go in parts, each part's best to the workspace, and a second launch chooses among them.
+// Rows that are longer than that go in parts, each part's best to the workspace, and a second launch chooses among them.
 #include <algorithm>
 
 #include "operators.h"
@@ -17,7 +17,7 @@ namespace ens {
 enum { TOP_VALUE = 0, TOP_LOG = 1, TOP_LOG_SOFTMAX = 2 };
 constexpr int TOP_ROOM = 1024, TOP_WAVE_ROOM = 256;     // candidates in LDS
 constexpr int TOP_WAVE_K = 32;                          // for which the 64 lanes of a wavefront are groups enough
-constexpr int JOIN_THREADS = 256, JOIN_KEYS = 2048;     // keys of a row's parts: 8 a thread, so that 128 threads' keys have room
+constexpr int JOIN_THREADS = 1024, JOIN_KEYS = 2048;    // keys of a row's parts: 8 for each of 256 groups, so that those of 128 groups have room
 
 __device__ __forceinline__ uint32_t key_of(float v) { return v != v ? 0u : ordered(v + 0.f); }      // both zeros are one
 __device__ __forceinline__ float value_of(uint32_t key) { return key == 0u ? __uint_as_float(0x7FC00000u) : unordered(key); }
@@ -95,25 +95,31 @@ __device__ __attribute__((noinline)) int halve(const T* p, int len, int base, in
     return above < k ? k : above;
 }
 
-// Calls f(rank, key) for the best k of `have` different keys in LDS, in no order.  Sixteen of them are read ahead of the comparisons, which would
-// otherwise wait for each (8 us of 17 for one row of 128 000 classes); there is room for zeros behind the last.
+// Calls f(rank, key) for the best k of `have` different keys in LDS, in no order.  Up to eight threads share a key's comparisons, and read sixteen keys
+// ahead of them, which would otherwise wait for each; there is room for zeros behind the last key.
 constexpr int AHEAD = 16;
 template <int THREADS, class F>
 __device__ __forceinline__ void rank_keys(uint64_t* found, int have, int k, F f) {
-    const int padded = (have + AHEAD - 1) / AHEAD * AHEAD;
-    if ((int)threadIdx.x < padded - have) found[have + threadIdx.x] = 0;
+    const int padded = (have + AHEAD - 1) / AHEAD * AHEAD, tid = threadIdx.x;
+    if (tid < padded - have) found[have + tid] = 0;
     group_sync<THREADS>();
-    for (int i = threadIdx.x; i < have; i += THREADS) {
-        const uint64_t one = found[i];
+    int share = 1;
+    if constexpr (THREADS > 64)
+        while (share < 8 && 2 * share * have <= THREADS) share *= 2;
+    for (int first = 0; first < have; first += THREADS / share) {
+        const int i = first + tid / share;
+        const uint64_t one = i < have ? found[i] : 0;
         int at = 0;
-        for (int o = 0; o < padded; o += AHEAD) {
+        for (int o = tid % share * AHEAD; o < padded; o += share * AHEAD) {
             uint64_t other[AHEAD];
 #pragma unroll
             for (int e = 0; e < AHEAD; e++) other[e] = found[o + e];
 #pragma unroll
             for (int e = 0; e < AHEAD; e++) at += other[e] > one;
         }
-        if (at < k) f(at, one);
+        if constexpr (THREADS > 64)
+            for (int o = 1; o < share; o *= 2) at += __shfl_xor(at, o, 64);
+        if (i < have && tid % share == 0 && at < k) f(at, one);
     }
 }
 
@@ -125,14 +131,15 @@ struct TopParts {
 };
 
 template <class T, int THREADS, int PIECES, bool LSE>
-__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
+__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
     constexpr int ROOM = THREADS == 64 ? TOP_WAVE_ROOM : TOP_ROOM, MOST = THREADS < 256 ? THREADS : 256;
+    constexpr bool AGAIN = PIECES > 4;
     __shared__ __align__(16) uint64_t found[ROOM + AHEAD];
     __shared__ __align__(16) float maxima[MOST];
     __shared__ float box[16];
     __shared__ uint32_t bound;
-    __shared__ int count;
-    const int tid = threadIdx.x, k = a.k;
+    __shared__ int count, listed, shares[AGAIN ? THREADS : 1];
+    const int tid = threadIdx.x, lane = tid & 63, k = a.k;
     const int groups = THREADS == 64 || k <= 32 ? 64 : k <= 64 ? 128 : 256;    // twice k, so that few values exceed the bound
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = split.parts == 1 ? job : job / split.parts;
@@ -147,23 +154,26 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         const int member = THREADS / groups;
         if (tid % member == 0) maxima[tid / member] = folded;
         if (tid == 0) {
-            count = 0;
             bound = 0;
+            count = 0;
+            listed = 0;
         }
         group_sync<THREADS>();
-        if (tid < groups) {
-            const float mine = maxima[tid];
+        {
+            // the lanes of a group share its comparisons; the k-th largest maximum is the largest that k of them reach
+            const int some = groups / member;
+            const float* const theirs = maxima + tid % member * some;
             int no_smaller = 0;
-            for (int i = 0; i < groups; i += 2 * AHEAD) {
-                float4 m[AHEAD / 2];
+            for (int i = 0; i < some; i += AHEAD / 2) {
+                float4 m[AHEAD / 8];
 #pragma unroll
-                for (int e = 0; e < AHEAD / 2; e++) m[e] = *(const float4*)&maxima[i + 4 * e];
+                for (int e = 0; e < AHEAD / 8; e++) m[e] = *(const float4*)&theirs[i + 4 * e];
 #pragma unroll
-                for (int e = 0; e < AHEAD / 2; e++) no_smaller += (m[e].x >= mine) + (m[e].y >= mine) + (m[e].z >= mine) + (m[e].w >= mine);
+                for (int e = 0; e < AHEAD / 8; e++) no_smaller += (m[e].x >= folded) + (m[e].y >= folded) + (m[e].z >= folded) + (m[e].w >= folded);
             }
-            // the k-th largest is the largest that k of them reach
-            const float reached = lanes_max(no_smaller >= k ? mine : LOWEST);
-            if ((tid & 63) == 0) atomicMax(&bound, key_of(reached));
+            for (int o = 1; o < member; o <<= 1) no_smaller += __shfl_xor(no_smaller, o, 64);
+            const float reached = lanes_max(no_smaller >= k ? folded : LOWEST);
+            if (lane == 0) atomicMax(&bound, key_of(reached));
         }
         float mx = LOWEST, sum = 0.f;
         if (LSE) {
@@ -179,22 +189,45 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         }
         group_sync<THREADS>();
         const float t = value_of(bound);
-        if (held.at >= 0 && held.one >= t) {
+        auto take = [&](float v, int c) {
+            if (!(v >= t)) return;
             const int at = atomicAdd(&count, 1);
-            if (at < ROOM) found[at] = key_of(held.one, first + held.at);
-        }
-        held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
-            float most = v[0];
+            if (at < ROOM) found[at] = key_of(v, first + c);
+        };
+        if (held.at >= 0) take(held.one, held.at);
+        if constexpr (AGAIN) {
+            // some k threads hold one: sixteen threads each read such a thread's pieces again, from the cache
+            if (own >= t) shares[atomicAdd(&listed, 1)] = tid;
+            __syncthreads();
+            const int piece = tid % 16 * THREADS;
+            for (int i = tid / 16; i < listed; i += 4 * (THREADS / 16)) {
+                uint4 u[4];
+                int at[4];
 #pragma unroll
-            for (int e = 1; e < PIECE<T>; e++) most = fmaxf(most, v[e]);
-            if (!(most >= t) || tid >= x.pieces - piece) return;
-#pragma unroll
-            for (int e = 0; e < PIECE<T>; e++)
-                if (v[e] >= t) {
-                    const int at = atomicAdd(&count, 1);
-                    if (at < ROOM) found[at] = key_of(v[e], first + x.head + (piece + tid) * PIECE<T> + e);
+                for (int e = 0; e < 4; e++) {
+                    const int s = i + e * (THREADS / 16);
+                    at[e] = s < listed ? piece + shares[s] : x.pieces;
+                    if (at[e] < x.pieces) u[e] = x.body()[at[e]];
                 }
-        });
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (at[e] < x.pieces) {
+                        float v[PIECE<T>];
+                        unpack(u[e], v, p);
+#pragma unroll
+                        for (int j = 0; j < PIECE<T>; j++) take(v[j], x.head + at[e] * PIECE<T> + j);
+                    }
+            }
+        } else {
+            held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
+                float most = v[0];
+#pragma unroll
+                for (int e = 1; e < PIECE<T>; e++) most = fmaxf(most, v[e]);
+                if (!(most >= t) || tid >= x.pieces - piece) return;
+#pragma unroll
+                for (int e = 0; e < PIECE<T>; e++) take(v[e], x.head + (piece + tid) * PIECE<T> + e);
+            });
+        }
         group_sync<THREADS>();
         int have = count;
         const int want = min(k, length);
@@ -216,27 +249,23 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
     }
 }
 
-// Among the keys that the parts of a row left.  They are dealt to the threads in turn, so that a part's best are with as many threads; k of
-// the threads' maxima reach the k-th largest of them, and what those threads hold has room.
+// Among the keys that the parts of a row left.  They are dealt to groups of four threads in turn, so that a part's best are with as many groups; k of
+// the groups' maxima reach the k-th largest of them, and what those groups hold has room.
 template <bool LSE>
 __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(const TopArgs a, const TopParts split) {
-    __shared__ __align__(16) uint64_t found[JOIN_KEYS / JOIN_THREADS * TOP_MAX_K + AHEAD], maxima[JOIN_THREADS];
+    constexpr int EACH = JOIN_KEYS / JOIN_THREADS, GROUPS = 256, MEMBER = JOIN_THREADS / GROUPS;
+    __shared__ __align__(16) uint64_t found[JOIN_KEYS / GROUPS * TOP_MAX_K + AHEAD], maxima[GROUPS];
     __shared__ uint64_t bound;
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, k = a.k;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const uint64_t* const in = (const uint64_t*)a.workspace + row * split.parts * k;
-        uint64_t mine[JOIN_KEYS / JOIN_THREADS], best = 0;
+        uint64_t mine[EACH], best = 0;
 #pragma unroll
-        for (int i = 0; i < JOIN_KEYS / JOIN_THREADS; i++) {
-            const int at = i * JOIN_THREADS + tid;
+        for (int i = 0; i < EACH; i++) {
+            const int at = (i * MEMBER + tid % MEMBER) * GROUPS + tid / MEMBER;
             mine[i] = at < split.parts * k ? in[at] : 0;
             best = mine[i] > best ? mine[i] : best;
-        }
-        maxima[tid] = best;
-        if (tid == 0) {
-            count = 0;
-            bound = 0;
         }
         float mx = LOWEST, sum = 0.f;
         if (LSE) {                                               // every wavefront for itself
@@ -247,20 +276,33 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(const TopArgs a,
             for (int i = lane; i < split.parts; i += 64) sum += from[i].y * __builtin_amdgcn_exp2f((from[i].x - mx) * power.c);
             sum = lanes_sum(sum);
         }
+#pragma unroll
+        for (int o = 1; o < MEMBER; o *= 2) {
+            const uint64_t other = __shfl_xor(best, o, 64);
+            best = other > best ? other : best;
+        }
+        if (tid % MEMBER == 0) maxima[tid / MEMBER] = best;
+        if (tid == 0) {
+            count = 0;
+            bound = 0;
+        }
         __syncthreads();
         int larger = 0;
-        for (int i = 0; i < JOIN_THREADS; i += AHEAD) {
+#pragma unroll
+        for (int i = 0; i < GROUPS / MEMBER; i += AHEAD) {
             uint64_t other[AHEAD];
 #pragma unroll
-            for (int e = 0; e < AHEAD; e++) other[e] = maxima[i + e];
+            for (int e = 0; e < AHEAD; e++) other[e] = maxima[tid % MEMBER * (GROUPS / MEMBER) + i + e];
 #pragma unroll
             for (int e = 0; e < AHEAD; e++) larger += other[e] > best;
         }
-        if (larger == k - 1 && best) bound = best;               // (fewer than k threads with keys: all keys)
+#pragma unroll
+        for (int o = 1; o < MEMBER; o *= 2) larger += __shfl_xor(larger, o, 64);
+        if (larger == k - 1 && best && tid % MEMBER == 0) bound = best;      // (fewer than k groups with keys: all keys)
         __syncthreads();
         const uint64_t t = bound ? bound : 1;
 #pragma unroll
-        for (int i = 0; i < JOIN_KEYS / JOIN_THREADS; i++)
+        for (int i = 0; i < EACH; i++)
             if (mine[i] >= t) found[atomicAdd(&count, 1)] = mine[i];
         __syncthreads();
         const float shift = LSE ? sum == 0.f ? 0.f : logf(sum) : 0.f;
@@ -303,19 +345,20 @@ __global__ __launch_bounds__(1024) void top_long_kernel(const TopArgs a) {
     }
 }
 
-// How a call's rows are cut; parts 0: too long.
-static TopParts split_top(int64_t n, int classes, int k, int dtype) {
-    const int piece = dtype == 0 ? 4 : 8, pieces = classes / piece;
-    const int most = std::max(1, JOIN_KEYS / k);
-    int parts = 1;
-    if (n < 256 && pieces > 1024) parts = std::min<int64_t>({(pieces + 511) / 512, most, std::max<int64_t>(1, 1024 / n)});
-    if (pieces > 16384) parts = std::max(parts, (pieces + 8191) / 8192);
-    if (parts > most) return TopParts{0, 0};
+// How rows are cut; parts 0: too long.  A row that a workgroup's registers hold stays whole, also where there is only one: 128 000 bf16 classes take
+// 12.8 us whole, as a call from Python, and 16 in 32 parts with the second launch; 32 000 take 11.3 and 15.3, and of 64 and 200 rows 11.3 to
+// 20 and 18 to 31.
+static TopParts split_top(int classes, int k, int dtype) {
+    const int pieces = classes / (dtype == 0 ? 4 : 8), parts = pieces > 16384 ? (pieces + 8191) / 8192 : 1;
+    if (parts > std::max(1, JOIN_KEYS / k)) return TopParts{0, 0};
     const int length = ((classes + parts - 1) / parts + 63) / 64 * 64;
     return TopParts{(classes + length - 1) / length, length};
 }
 
-int64_t top_workspace(int64_t n, int classes, int k, int dtype) { return split_top(n, classes, k, dtype).parts ? split_top(n, classes, k, dtype).bytes(n, k) : 0; }
+int64_t top_workspace(int64_t n, int classes, int k, int dtype) {
+    const TopParts split = split_top(classes, k, dtype);
+    return split.parts ? split.bytes(n, k) : 0;
+}
 
 template <class T, int THREADS, int PIECES>
 static void launch_top_held(const TopArgs& a, const TopParts& split, hipStream_t s) {
@@ -325,7 +368,7 @@ static void launch_top_held(const TopArgs& a, const TopParts& split, hipStream_t
 }
 
 hipError_t launch_top(const TopArgs& a, hipStream_t s) {
-    const TopParts split = split_top(a.n, a.classes, a.k, a.dtype);
+    const TopParts split = split_top(a.classes, a.k, a.dtype);
     return by_type(a.dtype, [&](auto t) {
         typedef decltype(t) T;
         const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 14));
