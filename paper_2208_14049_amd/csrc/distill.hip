@@ -15,6 +15,7 @@
 namespace ens {
 
 constexpr int KEPT_LANES = DISTILL_MAX_K / 64;
+constexpr int CUS = 256;                                         // compute units
 
 // The teacher's record of a row in LDS, as a wavefront leaves it: class (or -1) and q of k entries, the sum of q, q_0, and the sum of q ln q.
 struct Record {
@@ -123,7 +124,7 @@ static __host__ __device__ int record_words(int k) { return 16 + 2 * k + 3; }
 
 // A workgroup a row, the row in registers between its maximum, its sums and its gradient.
 template <class T, bool TAIL, int THREADS, int PIECES>
-__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void distill_held_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void distill_held_kernel(const DistillArgs a) {
     extern __shared__ int lds[];
     const int tid = threadIdx.x, k = a.k;
     float* const box = (float*)lds;
@@ -398,7 +399,8 @@ static hipError_t launch_distill_as(const DistillArgs& a, hipStream_t s) {
         if (pieces <= 64 * 4) return launch_held<T, TAIL, 64, 4>(a, s);
         if (pieces <= 256 * 4) return launch_held<T, TAIL, 256, 4>(a, s);
         if (pieces <= 256 * 8) return launch_held<T, TAIL, 256, 8>(a, s);
-        if (pieces <= 512 * 8) return launch_held<T, TAIL, 512, 8>(a, s);
+        if (pieces <= 256 * 16) return launch_held<T, TAIL, 256, 16>(a, s);
+        if (pieces <= 256 * 28 && 3 * ((a.n + 3 * CUS - 1) / (3 * CUS)) <= 2 * ((a.n + 2 * CUS - 1) / (2 * CUS))) return launch_held<T, TAIL, 256, 28>(a, s);
         if (pieces <= 512 * 16) return launch_held<T, TAIL, 512, 16>(a, s);
         return launch_held<T, TAIL, 1024, 16>(a, s);
     }

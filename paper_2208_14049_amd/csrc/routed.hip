@@ -134,7 +134,7 @@ __device__ __forceinline__ float inverse_sum(const Exp& power, float ln_sum) { r
 // A workgroup for a row and a member (BY_MEMBER: the member's gradient, zeros where the row did not choose it) or for a row and a choice (the
 // weights' gradients alone).  The jobs of a row go to one XCD, one after the other, so that the row of g is read from memory once.
 template <class T, int THREADS, int PIECES, bool BY_MEMBER>
-__global__ __launch_bounds__(THREADS) void combine_routed_backward_kernel(const RoutedArgs a, const int64_t jobs) {
+__global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_backward_kernel(const RoutedArgs a, const int64_t jobs) {
     __shared__ float box[16];
     const int tid = threadIdx.x, lane = tid & 63, classes = a.classes;
     const int per_row = BY_MEMBER ? a.members : a.k;

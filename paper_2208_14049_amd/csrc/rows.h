@@ -156,6 +156,7 @@ struct Row {
     }
 };
 
+typedef uint32_t Quad __attribute__((ext_vector_type(4)));
 // The compiler takes u for a new value from here on: it would keep the unpacked values of a row from one use of it to the next, in twice the registers.
 __device__ __forceinline__ void renew(uint4& u) { asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
 
@@ -212,7 +213,7 @@ struct Held {
             char* const to = (char*)(dst + x.head + piece * PIECE<T>);
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) v[e] = f(v[e]);
-            if (alike) *(uint4*)(to + mine) = pack(v, x.p);
+            if (alike) __builtin_nontemporal_store(__builtin_bit_cast(Quad, pack(v, x.p)), (Quad*)(to + mine));
             else
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) *(T*)(to + mine + e * sizeof(T)) = (T)v[e];

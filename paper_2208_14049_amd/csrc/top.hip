@@ -131,7 +131,7 @@ struct TopParts {
 };
 
 template <class T, int THREADS, int PIECES, bool LSE>
-__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
+__global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
     constexpr int ROOM = THREADS == 64 ? TOP_WAVE_ROOM : TOP_ROOM, MOST = THREADS < 256 ? THREADS : 256;
     constexpr bool AGAIN = PIECES > 4;
     __shared__ __align__(16) uint64_t found[ROOM + AHEAD];
@@ -196,16 +196,17 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) vo
         };
         if (held.at >= 0) take(held.one, held.at);
         if constexpr (AGAIN) {
-            // some k threads hold one: sixteen threads each read such a thread's pieces again, from the cache
+            // some k threads hold one: a thread for each of such a thread's pieces reads them again, from the cache
+            constexpr int EACH = PIECES, ROUND = THREADS / EACH;
             if (own >= t) shares[atomicAdd(&listed, 1)] = tid;
             __syncthreads();
-            const int piece = tid % 16 * THREADS;
-            for (int i = tid / 16; i < listed; i += 4 * (THREADS / 16)) {
+            const int piece = tid % EACH * THREADS;
+            for (int i = tid / EACH; i < listed; i += 4 * ROUND) {
                 uint4 u[4];
                 int at[4];
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    const int s = i + e * (THREADS / 16);
+                    const int s = i + e * ROUND;
                     at[e] = s < listed ? piece + shares[s] : x.pieces;
                     if (at[e] < x.pieces) u[e] = x.body()[at[e]];
                 }
@@ -380,7 +381,7 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
         const int pieces = split.length / PIECE<T>;
         if (pieces <= 64 * 4 && a.k <= TOP_WAVE_K) launch_top_held<T, 64, 4>(a, split, s);
         else if (pieces <= 256 * 4) launch_top_held<T, 256, 4>(a, split, s);
-        else if (pieces <= 512 * 8) launch_top_held<T, 512, 8>(a, split, s);
+        else if (pieces <= 256 * 16) launch_top_held<T, 256, 16>(a, split, s);
         else if (pieces <= 512 * 16) launch_top_held<T, 512, 16>(a, split, s);
         else launch_top_held<T, 1024, 16>(a, split, s);
         if (split.parts > 1) {
