@@ -39,6 +39,7 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
     __shared__ float box[16];
     const int tid = threadIdx.x, lane = tid & 63, classes = a.classes;
     const int one = Span<T, THREADS, PIECES>::single(classes, tid);
+    const bool past = a.n * classes >= 16 << 20;                 // 64 MiB: smaller outputs are in the caches for what reads them next
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         Choices choices(a, row, lane);
         float y[PIECES][PIECE<T>], y_one = 0.f;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
         if (one >= 0) out[one] = y_one;
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
-            if (tid < classes / PIECE<T> - i * THREADS) store_floats(out + (i * THREADS + tid) * PIECE<T>, y[i]);
+            if (tid < classes / PIECE<T> - i * THREADS) store_floats(out + (i * THREADS + tid) * PIECE<T>, y[i], past);
     }
 }
 
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
         if (!same || (!BY_MEMBER && __builtin_ctzll(same) != what)) {
             if (!out) continue;
             if (one >= 0) out[one] = (T)0.f;
-            for (int i = tid; i < pieces; i += THREADS) store_loose(out + (int64_t)i * PIECE<T>, make_uint4(0, 0, 0, 0));
+            for (int i = tid; i < pieces; i += THREADS) store_past(out + (int64_t)i * PIECE<T>, make_uint4(0, 0, 0, 0));
             continue;
         }
         const int j = __builtin_ctzll(same);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
                     if (tid >= pieces - i * THREADS) return;
 #pragma unroll
                     for (int e = 0; e < PIECE<T>; e++) v[e] = scale * power(v[e]) * (g[i][e] - dot);
-                    store_loose((char*)(out + i * THREADS * PIECE<T>) + (uint32_t)tid * 16u, pack(v, out));
+                    store_past((char*)(out + i * THREADS * PIECE<T>) + (uint32_t)tid * 16u, pack(v, out));
                 });
             }
         } else {

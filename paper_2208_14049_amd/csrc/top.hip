@@ -140,7 +140,8 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
     __shared__ uint32_t bound;
     __shared__ int count, listed, shares[AGAIN ? THREADS : 1];
     const int tid = threadIdx.x, lane = tid & 63, k = a.k;
-    const int groups = THREADS == 64 || k <= 32 ? 64 : k <= 64 ? 128 : 256;    // twice k, so that few values exceed the bound
+    // twice k, so that few values exceed the bound; eight lanes of a group at most, which share eight comparisons and more
+    const int groups = THREADS == 64 ? 64 : max(k <= 32 ? 64 : k <= 64 ? 128 : 256, THREADS / 8);
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = split.parts == 1 ? job : job / split.parts;
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
