@@ -490,15 +490,27 @@ def _plain(t, device, shape, dtype, what):
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
+def _stream(device):
+    """Address of torch's current stream of a device: by the call that gives it as a number where torch has it (2 us less than a Stream object)."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(device.index)
+
+
 def _issue(device, name, *args):
     """A call on the current stream of a device."""
     from torch import cuda
     call = getattr(lib(), name)
     if device.index == cuda.current_device():
-        rc = call(*args, cuda.current_stream(device).cuda_stream)
+        rc = call(*args, _stream(device))
     else:
         with cuda.device(device):
-            rc = call(*args, cuda.current_stream(device).cuda_stream)
+            rc = call(*args, _stream(device))
     if rc != ENS_OK:
         raise EnsError(rc, name)
 
