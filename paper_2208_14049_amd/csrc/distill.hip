@@ -51,21 +51,37 @@ __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, i
 #pragma unroll
         for (int i = 0; i < KEPT_LANES; i++) q[i] *= scale;
     }
-    // the first entry of a class takes what the later ones have
+    // does a class come twice?
+    bool twice = false;
+#pragma unroll
+    for (int o = 0; o < KEPT_LANES; o++) {
+        const int entries = min(64, a.k - 64 * o);
+        for (int l = 0; l < entries; l++) {
+            const int other = __builtin_amdgcn_readlane(c[o], l);
+            int same = 0;
+#pragma unroll
+            for (int i = 0; i < KEPT_LANES; i++)
+                if (64 * i < a.k) same += __popcll(__ballot(c[i] == other));
+            twice = twice || (same > 1 && other >= 0);
+        }
+    }
     float mass = 0.f, entropy = 0.f;
 #pragma unroll
     for (int i = 0; i < KEPT_LANES; i++) {
         if (64 * i >= a.k) break;
         const int j = 64 * i + lane;
-        float all = 0.f;
+        float all = q[i];
         bool first = c[i] >= 0;
+        if (twice) {                                             // the first entry of a class takes what the later ones have
+            all = 0.f;
 #pragma unroll
-        for (int o = 0; o < KEPT_LANES; o++) {
-            const int entries = min(64, a.k - 64 * o);
-            for (int l = 0; l < entries; l++) {
-                const bool same = c[i] == __builtin_amdgcn_readlane(c[o], l);
-                all += same ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q[o]), l)) : 0.f;
-                if (64 * o + l < j) first = first && !same;
+            for (int o = 0; o < KEPT_LANES; o++) {
+                const int entries = min(64, a.k - 64 * o);
+                for (int l = 0; l < entries; l++) {
+                    const bool same = c[i] == __builtin_amdgcn_readlane(c[o], l);
+                    all += same ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q[o]), l)) : 0.f;
+                    if (64 * o + l < j) first = first && !same;
+                }
             }
         }
         if (!first) all = 0.f;

@@ -130,6 +130,81 @@ struct TopParts {
     __host__ __device__ int64_t bytes(int64_t n, int k) const { return parts == 1 ? 0 : 8 * (keys(n, k) + n * parts); }
 };
 
+// The k-th largest of the maxima of `groups` groups of lanes, as a bound: `own` is the largest of this thread's values.  A group is up to eight
+// neighbouring lanes, which share its comparisons.  *bound is 0 before.
+template <int THREADS>
+__device__ __forceinline__ float find_bound(float own, int groups, int k, float* maxima, uint32_t* bound) {
+    const int tid = threadIdx.x, member = THREADS / groups, some = groups / member;
+    float folded = own;
+    for (int o = 1; o < member; o <<= 1) folded = fmaxf(folded, __shfl_xor(folded, o, 64));
+    if (tid % member == 0) maxima[tid / member] = folded;
+    group_sync<THREADS>();
+    const float* const theirs = maxima + tid % member * some;
+    int no_smaller = 0;
+    for (int i = 0; i < some; i += AHEAD / 2) {
+        float4 m[AHEAD / 8];
+#pragma unroll
+        for (int e = 0; e < AHEAD / 8; e++) m[e] = *(const float4*)&theirs[i + 4 * e];
+#pragma unroll
+        for (int e = 0; e < AHEAD / 8; e++) no_smaller += (m[e].x >= folded) + (m[e].y >= folded) + (m[e].z >= folded) + (m[e].w >= folded);
+    }
+    for (int o = 1; o < member; o <<= 1) no_smaller += __shfl_xor(no_smaller, o, 64);
+    const float reached = lanes_max(no_smaller >= k ? folded : LOWEST);      // the largest that k of them reach
+    if ((tid & 63) == 0) atomicMax(bound, key_of(reached));
+    group_sync<THREADS>();
+    return value_of(*bound);
+}
+
+// Short rows for many of their values: fewer pieces of 16 bytes than twice k.  The values are dealt to the threads one by one, so that each has one of the
+// row's parts; otherwise as below.
+template <class T, int THREADS, int EACH, bool LSE>
+__global__ __launch_bounds__(THREADS) void top_dealt_kernel(const TopArgs a) {
+    constexpr int ROOM = THREADS == 64 ? TOP_WAVE_ROOM : TOP_ROOM;
+    __shared__ __align__(16) uint64_t found[ROOM + AHEAD];
+    __shared__ __align__(16) float maxima[THREADS];
+    __shared__ float box[16];
+    __shared__ uint32_t bound;
+    __shared__ int count;
+    const int tid = threadIdx.x, k = a.k;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const T* const p = (const T*)a.values + row * a.ld;
+        float v[EACH], own = LOWEST;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) v[i] = tid + i * THREADS < a.classes ? up(p[tid + i * THREADS]) : NONE;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) own = fmaxf(own, v[i]);
+        if (tid == 0) {
+            bound = 0;
+            count = 0;
+        }
+        const float t = find_bound<THREADS>(own, THREADS, k, maxima, &bound);
+        float mx = LOWEST, sum = 0.f;
+        if (LSE) {
+            mx = group_max<THREADS>(own, box);
+            const Exp power(mx, a.inv_temperature);
+#pragma unroll
+            for (int i = 0; i < EACH; i++) sum += power(v[i]);
+            sum = group_sum<THREADS>(sum, box) * power.off();
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; i++)
+            if (v[i] >= t && tid + i * THREADS < a.classes) {
+                const int at = atomicAdd(&count, 1);
+                if (at < ROOM) found[at] = key_of(v[i], tid + i * THREADS);
+            }
+        group_sync<THREADS>();
+        int have = count;
+        if (have > ROOM || have < k) have = halve<T, THREADS>(p, a.classes, 0, k, ROOM, found, &count, box);
+        const float shift = LSE ? sum == 0.f ? 0.f : logf(sum) : 0.f;
+        rank_keys<THREADS>(found, have, k, [&](int at, uint64_t key) {
+            const float x = value_of((uint32_t)(key >> 32));
+            a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+            a.value[row * k + at] = LSE ? (x - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(x) : x;
+        });
+        group_sync<THREADS>();
+    }
+}
+
 template <class T, int THREADS, int PIECES, bool LSE>
 __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel(const TopArgs a, const TopParts split) {
     constexpr int ROOM = THREADS == 64 ? TOP_WAVE_ROOM : TOP_ROOM, MOST = THREADS < 256 ? THREADS : 256;
@@ -139,43 +214,23 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
     __shared__ float box[16];
     __shared__ uint32_t bound;
     __shared__ int count, listed, shares[AGAIN ? THREADS : 1];
-    const int tid = threadIdx.x, lane = tid & 63, k = a.k;
-    // twice k, so that few values exceed the bound; eight lanes of a group at most, which share eight comparisons and more
-    const int groups = THREADS == 64 ? 64 : max(k <= 32 ? 64 : k <= 64 ? 128 : 256, THREADS / 8);
+    const int tid = threadIdx.x, k = a.k;
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = split.parts == 1 ? job : job / split.parts;
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
         const T* const p = (const T*)a.values + row * a.ld + first;
         const Row<T, THREADS> x(p, length);
+        // twice k, so that few values exceed the bound; as many as there are where not all threads have a piece; eight lanes of a group at most
+        const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : max(k <= 32 ? 64 : k <= 64 ? 128 : 256, THREADS / 8);
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
         const float own = held.max(x);                           // LOWEST for nothing but minus infinity
-        float folded = own;
-        for (int o = 1; o < THREADS / groups; o <<= 1) folded = fmaxf(folded, __shfl_xor(folded, o, 64));
-        const int member = THREADS / groups;
-        if (tid % member == 0) maxima[tid / member] = folded;
         if (tid == 0) {
             bound = 0;
             count = 0;
             listed = 0;
         }
-        group_sync<THREADS>();
-        {
-            // the lanes of a group share its comparisons; the k-th largest maximum is the largest that k of them reach
-            const int some = groups / member;
-            const float* const theirs = maxima + tid % member * some;
-            int no_smaller = 0;
-            for (int i = 0; i < some; i += AHEAD / 2) {
-                float4 m[AHEAD / 8];
-#pragma unroll
-                for (int e = 0; e < AHEAD / 8; e++) m[e] = *(const float4*)&theirs[i + 4 * e];
-#pragma unroll
-                for (int e = 0; e < AHEAD / 8; e++) no_smaller += (m[e].x >= folded) + (m[e].y >= folded) + (m[e].z >= folded) + (m[e].w >= folded);
-            }
-            for (int o = 1; o < member; o <<= 1) no_smaller += __shfl_xor(no_smaller, o, 64);
-            const float reached = lanes_max(no_smaller >= k ? folded : LOWEST);
-            if (lane == 0) atomicMax(&bound, key_of(reached));
-        }
+        const float t = find_bound<THREADS>(own, groups, k, maxima, &bound);
         float mx = LOWEST, sum = 0.f;
         if (LSE) {
             mx = group_max<THREADS>(own, box);
@@ -188,8 +243,6 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
             });
             sum = group_sum<THREADS>(sum + power(held.one), box) * power.off();
         }
-        group_sync<THREADS>();
-        const float t = value_of(bound);
         auto take = [&](float v, int c) {
             if (!(v >= t)) return;
             const int at = atomicAdd(&count, 1);
@@ -380,6 +433,17 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
             return hipGetLastError();
         }
         const int pieces = split.length / PIECE<T>;
+        if (pieces < 2 * a.k && a.classes <= (a.k <= TOP_WAVE_K ? 64 * 8 : 256 * 8)) {
+            const dim3 group(a.k <= TOP_WAVE_K ? 64 : 256);
+            if (a.k <= TOP_WAVE_K) {
+                if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_dealt_kernel<T, 64, 8, true>), rows, group, 0, s, a);
+                else hipLaunchKernelGGL((top_dealt_kernel<T, 64, 8, false>), rows, group, 0, s, a);
+            } else {
+                if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_dealt_kernel<T, 256, 8, true>), rows, group, 0, s, a);
+                else hipLaunchKernelGGL((top_dealt_kernel<T, 256, 8, false>), rows, group, 0, s, a);
+            }
+            return hipGetLastError();
+        }
         if (pieces <= 64 * 4 && a.k <= TOP_WAVE_K) launch_top_held<T, 64, 4>(a, split, s);
         else if (pieces <= 256 * 4) launch_top_held<T, 256, 4>(a, split, s);
         else if (pieces <= 256 * 16) launch_top_held<T, 256, 16>(a, split, s);
