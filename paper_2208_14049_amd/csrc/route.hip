@@ -262,6 +262,27 @@ __device__ __forceinline__ int best_of_keys(int k, int lane, uint32_t (&key)[PER
     return mine;
 }
 
+// By the gate's values themselves, those of them whose x is not minus infinity.
+template <class T, int PER>
+__device__ __forceinline__ int best_by_value(int k, int lane, const T (&raw)[PER], const float (&x)[PER]) {
+    if constexpr (sizeof(T) == 2) {
+        uint32_t key[PER];
+#pragma unroll
+        for (int j = 0; j < PER; j++) {
+            uint32_t b = bits_of(raw[j]) << 16;
+            b = b == 0x80000000u ? 0u : b;                       // both zeros are one
+            b ^= (uint32_t)((int32_t)b >> 31) | 0x80000000u;
+            key[j] = x[j] > NONE ? (b & 0xFFFF0000u) | (uint32_t)(0xFFFF - (lane * PER + j)) : 0u;
+        }
+        return best_of_keys<PER>(k, lane, key);
+    } else {
+        float c[PER];
+#pragma unroll
+        for (int j = 0; j < PER; j++) c[j] = x[j];
+        return best_in_order<float, PER>(k, lane, c);
+    }
+}
+
 // BY_VALUE: members rank by the gate's values themselves (no bias, no groups).
 template <class T, int PER, bool BY_VALUE>
 __global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route_kernel(const RouteArgs a) {
@@ -288,29 +309,29 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route
         }
         if (row + step < a.n) load_members(gates + step * a.ld, E, lane, (T)NONE, next);
         int mine;
-        if constexpr (BY_VALUE && sizeof(T) == 2) {
-            uint32_t key[PER];
-#pragma unroll
-            for (int j = 0; j < PER; j++) {
-                uint32_t b = bits_of(raw[j]) << 16;
-                b = b == 0x80000000u ? 0u : b;                   // both zeros are one
-                b ^= (uint32_t)((int32_t)b >> 31) | 0x80000000u;
-                key[j] = x[j] > NONE ? (b & 0xFFFF0000u) | (uint32_t)(0xFFFF - (lane * PER + j)) : 0u;
-            }
-            mine = best_of_keys<PER>(a.k, lane, key);
-        } else if constexpr (BY_VALUE) {
-            float c[PER];
-#pragma unroll
-            for (int j = 0; j < PER; j++) c[j] = x[j];
-            mine = best_in_order<float, PER>(a.k, lane, c);
-        } else {
+        bool told = true;
+        if (!BY_VALUE) {
             float c[PER], most, gap, apart = __builtin_inff();
             member_ranks<float, PER>(rule, lane, x, c, most);
             if (a.groups > 1) apart = drop_groups<float, PER>(rule, lane, c, (float*)ranks[wave]);
-            mine = best_members<PER>(a.k, lane, c, gap);
             // a score is off by some 20 units of 2^-24 of itself, a rank by half a unit of its own more, a sum of two by twice that
-            if (!(gap > fmaf(most, 0x1p-18f, 0x1p-120f) && apart > fmaf(most, 0x1p-16f, 0x1p-120f))) mine = choose_exactly<T, PER>(rule, gates, ranks[wave]);
+            told = apart > fmaf(most, 0x1p-16f, 0x1p-120f);
+            if (a.bias) {
+                mine = best_members<PER>(a.k, lane, c, gap);
+                told = told && gap > fmaf(most, 0x1p-18f, 0x1p-120f);
+            } else {
+                // members of the groups that stay, by value: scores rise with it, as far as they are not too small for 32 bits
+                bool small = false;
+#pragma unroll
+                for (int j = 0; j < PER; j++) {
+                    small = small || c[j] == 0.f;
+                    x[j] = c[j] > NONE ? x[j] : NONE;
+                }
+                told = told && __ballot(small) == 0;
+            }
         }
+        if (BY_VALUE || !a.bias) mine = best_by_value<T, PER>(a.k, lane, raw, x);
+        if (!told) mine = choose_exactly<T, PER>(rule, gates, ranks[wave]);
         const float own = mine >= 0 ? gate_value(up(gates[mine])) : NONE;
         float weight;
         if (a.renormalise) {
@@ -321,6 +342,8 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route
             weight = mine >= 0 ? sigmoid_of(own) : 0.f;
         } else {
             float m, sum;
+#pragma unroll
+            for (int j = 0; j < PER; j++) x[j] = gate_value(up(raw[j]));     // of all members, also of groups that do not stay
             softmax_of<float, PER>(x, m, sum);
             weight = mine >= 0 ? expf(own - m) / sum : 0.f;
         }

@@ -132,29 +132,26 @@ __global__ __launch_bounds__(LONG_THREADS) void combine_routed_long_kernel(const
 // What multiplies the terms of a member's row in its softmax: 1 / sum, 0 for a row that holds nothing.
 __device__ __forceinline__ float inverse_sum(const Exp& power, float ln_sum) { return ln_sum == NONE ? 0.f : expf(-ln_sum) * power.off(); }
 
-// A workgroup for a row and a member (BY_MEMBER: the member's gradient, zeros where the row did not choose it) or for a row and a choice (the
-// weights' gradients alone).  The jobs of a row go to one XCD, one after the other, so that the row of g is read from memory once.
+// A job is a row and a member (BY_MEMBER: the member's gradient, zeros where the row did not choose it) or a row and a choice (the weights'
+// gradients alone).  A workgroup of a long row has one, and the jobs of a row go to one XCD, one after the other, so that the row of g is read from memory
+// once; a wavefront takes all the jobs of a row of one piece a lane (8 100 rows of 10 classes, three of twelve members: 15 us instead of 30, as a call from
+// Python; of 1 000 classes 93 instead of 87).
 template <class T, int THREADS, int PIECES, bool BY_MEMBER>
 __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_backward_kernel(const RoutedArgs a, const int64_t jobs) {
     __shared__ float box[16];
     const int tid = threadIdx.x, lane = tid & 63, classes = a.classes;
     const int per_row = BY_MEMBER ? a.members : a.k;
     const int one = Span<T, THREADS, PIECES>::single(classes, tid), pieces = classes / PIECE<T>;
-    for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int64_t eights = job / 8;
-        const int64_t row = eights / per_row * 8 + job % 8;
-        if (row >= a.n) continue;
-        const int what = (int)(eights % per_row);
-        const Choices choices(a, row, lane);
+    auto one_job = [&](const int64_t row, const Choices& choices, const int what) {
         const int m = BY_MEMBER ? what : __builtin_amdgcn_readlane(choices.member, what);
         if (a.d_weights && what == 0 && tid < a.k && choices.member < 0) a.d_weights[row * a.k + tid] = 0.f;
         const uint64_t same = m < 0 ? 0 : choices.of(m);
         T* const out = BY_MEMBER && a.d_logits[m] ? (T*)a.d_logits[m] + row * a.ld_d : nullptr;
         if (!same || (!BY_MEMBER && __builtin_ctzll(same) != what)) {
-            if (!out) continue;
+            if (!out) return;
             if (one >= 0) out[one] = (T)0.f;
             for (int i = tid; i < pieces; i += THREADS) store_past(out + (int64_t)i * PIECE<T>, make_uint4(0, 0, 0, 0));
-            continue;
+            return;
         }
         const int j = __builtin_ctzll(same);
         const T* const z_row = (const T*)a.logits[m] + row * a.ld;
@@ -210,6 +207,17 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
             if (out) walk([&](float v, float g, int64_t c) { out[c] = (T)(scale * power(v) * (g - dot)); });
         }
         if (a.d_weights && tid < 64 && same >> lane & 1) a.d_weights[row * a.k + lane] = dot;
+    };
+    if constexpr (PIECES == 1) {
+        for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+            const Choices choices(a, row, lane);
+            for (int what = 0; what < per_row; what++) one_job(row, choices, what);
+        }
+    } else {
+        for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+            const int64_t eights = job / 8, row = eights / per_row * 8 + job % 8;
+            if (row < a.n) one_job(row, Choices(a, row, lane), (int)(eights % per_row));
+        }
     }
 }
 
@@ -218,7 +226,8 @@ hipError_t launch_combine_routed(const RoutedArgs& a, hipStream_t s) {
         typedef decltype(t) T;
         const int pieces = (a.classes + PIECE<T> - 1) / PIECE<T>;
         const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 16));
-        if (pieces <= 64 * 4) hipLaunchKernelGGL((combine_routed_kernel<T, 64, 4>), rows, dim3(64), 0, s, a);
+        if (pieces <= 64) hipLaunchKernelGGL((combine_routed_kernel<T, 64, 1>), rows, dim3(64), 0, s, a);
+        else if (pieces <= 64 * 4) hipLaunchKernelGGL((combine_routed_kernel<T, 64, 4>), rows, dim3(64), 0, s, a);
         else if (pieces <= 256 * 4) hipLaunchKernelGGL((combine_routed_kernel<T, 256, 4>), rows, dim3(256), 0, s, a);
         else if (pieces <= 512 * 8) hipLaunchKernelGGL((combine_routed_kernel<T, 512, 8>), rows, dim3(512), 0, s, a);
         else if (pieces <= 1024 * 8) hipLaunchKernelGGL((combine_routed_kernel<T, 1024, 8>), rows, dim3(1024), 0, s, a);
@@ -232,7 +241,9 @@ static hipError_t launch_backward(const RoutedArgs& a, hipStream_t s) {
     const int pieces = (a.classes + PIECE<T> - 1) / PIECE<T>;
     const int64_t jobs = (a.n + 7) / 8 * 8 * (BY_MEMBER ? a.members : a.k);
     const dim3 grid((unsigned)std::min<int64_t>(jobs, 1 << 20));
-    if (pieces <= 64 * 4) hipLaunchKernelGGL((combine_routed_backward_kernel<T, 64, 4, BY_MEMBER>), grid, dim3(64), 0, s, a, jobs);
+    const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 16));
+    if (pieces <= 64) hipLaunchKernelGGL((combine_routed_backward_kernel<T, 64, 1, BY_MEMBER>), rows, dim3(64), 0, s, a, jobs);
+    else if (pieces <= 64 * 4) hipLaunchKernelGGL((combine_routed_backward_kernel<T, 64, 4, BY_MEMBER>), grid, dim3(64), 0, s, a, jobs);
     else if (pieces <= 256 * 4) hipLaunchKernelGGL((combine_routed_backward_kernel<T, 256, 4, BY_MEMBER>), grid, dim3(256), 0, s, a, jobs);
     else if (pieces <= 512 * 8) hipLaunchKernelGGL((combine_routed_backward_kernel<T, 512, 8, BY_MEMBER>), grid, dim3(512), 0, s, a, jobs);
     else hipLaunchKernelGGL((combine_routed_backward_kernel<T, LONG_THREADS, 0, BY_MEMBER>), grid, dim3(LONG_THREADS), 0, s, a, jobs);
