@@ -371,7 +371,8 @@ int ens_combine_routed_backward(const void* const* logits, int32_t dtype, int64_
  *   ENS_TOP_LOG_SOFTMAX  logarithms of the row's softmax at `temperature` (> 0; not read otherwise); minus
  *                        infinity in a row that holds nothing else
  * workspace: ens_top_workspace(...) bytes of device memory, 8-byte aligned, that nothing else uses until the
- * call's kernels have run (0 bytes: NULL).  ens_top_workspace returns a negative status for sizes that ens_top refuses. */
+ * call's kernels have run (0 bytes: NULL).  ens_top_workspace returns a negative status for sizes that ens_top refuses.  Up to
+ * 16 777 216 classes; rows that are too long for parts (1 000 000 bf16 classes at k = 128, more for less) are walked some thirty times. */
 enum { ENS_TOP_VALUE = 0, ENS_TOP_LOG = 1, ENS_TOP_LOG_SOFTMAX = 2 };
 int ens_top(const void* values, int32_t dtype, int64_t ld, int64_t n, int32_t classes, int32_t k, int32_t form, float temperature,
             int32_t* index, float* value, void* workspace, int64_t workspace_bytes, void* stream);
@@ -384,15 +385,15 @@ int64_t ens_top_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype);
  *   tail 0   q = softmax of log_probs over the entries;  loss = temperature^2 * sum_c q_c ln(q_c / p_c)
  *   tail 1   q = exp(log_probs), and what they leave of 1 (if anything) is one class more, which stands for all
  *            the classes without an entry: loss = temperature^2 * (sum_c q_c ln(q_c / p_c) + q_0 ln(q_0 / p_0)).
- *            262 144 classes at most.  Where the student gives the other classes nothing (none is left,
- *            or their logits are minus infinity) the tail counts nothing.
+ *            Where the student gives the other classes nothing (none is left, or their logits are minus
+ *            infinity) the tail counts nothing.
  * A row with no entry of any probability (tail 0), or whose logits are all minus infinity, has loss and gradient 0.
  *   loss     n;  state  n x 3 floats for the backward pass
  *   d_logits rows of dtype, ld_d apart, or NULL: the gradient of sum_i row_weights[i] * loss[i], in the same pass.
  *            It may be the logits themselves (with the same ld).  row_weights: n, or NULL for ones; a row of
  *            weight 0 gets zeros whatever its logits.
  *   workspace  ens_distill_workspace(...) bytes of device memory, 8-byte aligned, that nothing else uses until the
- *            call's kernels have run (0 bytes: NULL) */
+ *            call's kernels have run (0 bytes: NULL).  Up to 16 777 216 classes. */
 int ens_distill(const void* logits, int32_t dtype, int64_t ld, int64_t n, int32_t classes, const int32_t* index, const float* log_probs,
                 int32_t k, float temperature, int32_t tail, const float* row_weights, float* loss, float* state, void* d_logits, int64_t ld_d,
                 void* workspace, int64_t workspace_bytes, void* stream);

@@ -127,20 +127,20 @@ int ens_top(const void* values, int32_t dtype, int64_t ld, int64_t n, int32_t cl
     return status(launch_top(a, (hipStream_t)stream));
 }
 
-static int distill_sizes(int64_t n, int32_t classes, int32_t k, int32_t dtype, int32_t tail) {
+static int distill_sizes(int64_t n, int32_t classes, int32_t k, int32_t dtype) {
     if (n < 0 || classes < 1 || k < 1 || !element_bytes(dtype)) return ENS_E_INVALID;
-    if (k > DISTILL_MAX_K || classes > (tail ? TAIL_MAX : ROW_MAX)) return ENS_E_UNSUPPORTED;
+    if (k > DISTILL_MAX_K || classes > ROW_MAX) return ENS_E_UNSUPPORTED;
     return ENS_OK;
 }
 
 int64_t ens_distill_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype) {
-    const int rc = distill_sizes(n, classes, k, dtype, 0);
+    const int rc = distill_sizes(n, classes, k, dtype);
     return rc != ENS_OK || n == 0 ? rc : distill_workspace(n, classes, k, dtype);
 }
 
 static int distill_args(const void* logits, int32_t dtype, int64_t ld, int64_t n, int32_t classes, const int32_t* index, const float* log_probs,
                         int32_t k, float temperature, int32_t tail, const float* row_weights, DistillArgs* a) {
-    const int rc = distill_sizes(n, classes, k, dtype, tail);
+    const int rc = distill_sizes(n, classes, k, dtype);
     if (rc != ENS_OK) return rc;
     if (temperature_status(temperature) != ENS_OK) return temperature_status(temperature);
     *a = DistillArgs{};

@@ -11,7 +11,6 @@ constexpr int ROUTED_MAX_MEMBERS = 64, ROUTED_MAX_K = 64;
 constexpr int TOP_MAX_K = 128;
 constexpr int DISTILL_MAX_K = 256;
 constexpr int ROW_MAX = 1 << 24;             // classes of a row
-constexpr int TAIL_MAX = 1 << 18;            // of a row whose unlisted classes count as one: a bit of LDS each
 
 struct RouteArgs {
     const void* gates;           // n rows of `members` values, ld apart

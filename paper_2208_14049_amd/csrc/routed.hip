@@ -25,6 +25,10 @@ struct Choices {
         weight = member >= 0 ? a.weights[at] : 0.f;
         left = __ballot(member >= 0);
     }
+    // zeros where a choice is not there
+    __device__ __forceinline__ void clear_state(const RoutedArgs& a, int64_t row, int tid) const {
+        if (a.state && tid < a.k && member < 0) a.state[(row * a.k + tid) * 2] = a.state[(row * a.k + tid) * 2 + 1] = 0.f;
+    }
     __device__ __forceinline__ uint64_t of(int m) const { return __ballot(member == m); }
     // weights of the choices in the mask, in order
     __device__ __forceinline__ float sum(uint64_t mask) const {
@@ -42,6 +46,7 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
     const bool past = a.n * classes >= 16 << 20;                 // 64 MiB: smaller outputs are in the caches for what reads them next
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         Choices choices(a, row, lane);
+        choices.clear_state(a, row, tid);
         float y[PIECES][PIECE<T>], y_one = 0.f;
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
@@ -94,6 +99,7 @@ __global__ __launch_bounds__(LONG_THREADS) void combine_routed_long_kernel(const
     const int tid = threadIdx.x, lane = tid & 63;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         Choices choices(a, row, lane);
+        choices.clear_state(a, row, tid);
         uint64_t firsts = 0;
         while (choices.left) {
             const int j = __builtin_ctzll(choices.left), m = __builtin_amdgcn_readlane(choices.member, j);

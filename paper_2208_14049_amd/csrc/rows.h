@@ -137,23 +137,6 @@ struct Row {
             for (int e = 0; e < PIECE<T>; e++) f(v[e], head + i * PIECE<T> + e);
         }
     }
-    // The same, f(value, class) -> value to be stored at dst[class]; in 16-byte pieces where dst has the row's alignment.  dst may be p.
-    template <class F>
-    __device__ __forceinline__ void map(int tid, T* dst, F f) const {
-        const int one = single(tid);
-        if (one >= 0) dst[one] = (T)f(up(p[one]), one);
-        const bool alike = (((uintptr_t)dst - (uintptr_t)p) & 15u) == 0;
-        for (int i = tid; i < pieces; i += THREADS) {
-            float v[PIECE<T>];
-            unpack(body()[i], v, p);
-#pragma unroll
-            for (int e = 0; e < PIECE<T>; e++) v[e] = f(v[e], head + i * PIECE<T> + e);
-            if (alike) *(uint4*)(dst + head + i * PIECE<T>) = pack(v, p);
-            else
-#pragma unroll
-                for (int e = 0; e < PIECE<T>; e++) dst[head + i * PIECE<T> + e] = (T)v[e];
-        }
-    }
 };
 
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));

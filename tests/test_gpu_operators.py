@@ -333,6 +333,19 @@ def test_top_orders_and_masks(C, k):
         check_top(x[i:i + 1].cuda(), k)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,C,k", [(3, 300, 40), (200, 560, 95), (70, 2047, 128), (5, 100, 30), (2, 263000, 128), (3, 140001, 9), (2, 1100003, 128), (1, 3000001, 5)])
+def test_top_short_and_long(dtype, n, C, k):
+    """Rows with fewer 16-byte pieces than twice k, rows in parts, and rows that are too long for them."""
+    x = rows(n, C, TYPES[dtype], gen(C + k), 3.0, pad=1)
+    check_top(x, k)
+    check_top(x, k, "log_softmax", 1.3)
+    x[0] = -INF                                                  # a mask that leaves a few
+    x[0, ::C // 4] = 1.0
+    x[-1, C // 2:] = float("nan")
+    check_top(x, k)
+
+
 # ------------------------------------------------------------------------------------- distillation
 
 def record(n, C, k, g, mass=0.9):
@@ -384,7 +397,8 @@ def check_distill(logits, index, t, T=1.0, tail=False, row_weights=None):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("n,C,k,T", [(1, 1, 1, 1.0), (3, 2, 2, 2.0), (5, 10, 3, 1.0), (64, 1000, 5, 2.0), (7, 1001, 128, 1.0), (33, 513, 17, 4.0), (2, 4099, 256, 0.5),
-                                     (3, 33001, 50, 1.5), (1, 128000, 64, 1.0), (2, 150001, 100, 1.0), (300, 300, 20, 1.0), (1100, 77, 4, 1.0)])
+                                     (3, 33001, 50, 1.5), (1, 128000, 64, 1.0), (2, 150001, 100, 1.0), (300, 300, 20, 1.0), (1100, 77, 4, 1.0), (2, 600003, 30, 1.0),
+                                     (170, 70001, 3, 1.0), (8, 17001, 70, 1.0), (520, 45001, 2, 1.0), (9, 8200, 65, 1.0)])
 def test_distill(dtype, tail, n, C, k, T):
     g = gen(C + k)
     logits = rows(n, C, TYPES[dtype], g, 2.0, pad=5, start=3)

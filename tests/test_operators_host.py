@@ -87,8 +87,8 @@ UNSUPPORTED = [
     (combine, dict(members=65, logits=pointers(*[P] * 65))), (combine, dict(k=65)), (combine, dict(classes=(1 << 24) + 1, ld=1 << 25)),
     (top, dict(temperature=2.0 ** -21)), (top, dict(temperature=2.0 ** 21)), (distill, dict(temperature=1e-9)), (distill_backward, dict(temperature=1e9)),
     (top, dict(k=129, classes=1000, ld=1000)), (top, dict(classes=(1 << 24) + 1, ld=1 << 25)),
-    (distill, dict(k=257)), (distill, dict(classes=(1 << 24) + 1, ld=1 << 25)), (distill, dict(classes=(1 << 18) + 1, ld=1 << 19, tail=1)),
-    (distill_backward, dict(classes=(1 << 18) + 1, ld=1 << 19, ld_d=1 << 19, tail=1)),
+    (distill, dict(k=257)), (distill, dict(classes=(1 << 24) + 1, ld=1 << 25)),
+    (distill_backward, dict(classes=(1 << 24) + 1, ld=1 << 25, ld_d=1 << 25, tail=1)),
 ]
 
 
