@@ -101,15 +101,17 @@ __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, i
     }
 }
 
-// A bit for each class, set for those that are kept: bit PIECE + c - head, so that a piece's bits stand together, in a byte or half a byte.
+// A bit for each class, set for those that are kept: bit HEADS + c - head, so that a piece's bits stand together, in a byte or half a byte.
 // Piece `first` + tid, `first` even.
-template <class T>
+template <class T, int THREADS>
 __device__ __forceinline__ uint32_t piece_marks(const uint32_t* marks, int first, int tid) {
     const uint8_t* const bytes = (const uint8_t*)marks;
-    if constexpr (PIECE<T> == 8) return bytes[tid + 1 + first];
-    else return bytes[((tid + 1) >> 1) + (first >> 1)] >> (4 * ((tid + 1) & 1)) & 15u;
+    constexpr int HEADS = Row<T, THREADS>::HEADS;
+    if constexpr (PIECE<T> == 8) return bytes[HEADS / 8 + tid + first];
+    else return bytes[((HEADS / 4 + tid) >> 1) + (first >> 1)] >> (4 * ((HEADS / 4 + tid) & 1)) & 15u;
 }
-static __host__ __device__ int mark_words(int pieces, int piece) { return ((pieces + 2) * piece + 31) / 32; }
+template <class T, int THREADS>
+static __host__ __device__ int mark_words(int pieces) { return ((pieces + 1) * PIECE<T> + Row<T, THREADS>::HEADS + 31) / 32; }
 
 // e of a piece into the sums over kept classes and others
 template <int N>
@@ -153,11 +155,11 @@ __global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIEC
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
         if (TAIL)
-            for (int i = tid; i < mark_words(THREADS * PIECES, PIECE<T>); i += THREADS) marks[i] = 0;
+            for (int i = tid; i < mark_words<T, THREADS>(THREADS * PIECES); i += THREADS) marks[i] = 0;
         if (tid < 64) read_record(a, row, tid, record);
         group_sync<THREADS>();
         float at_kept[(DISTILL_MAX_K + THREADS - 1) / THREADS];
-        const int shift = PIECE<T> - x.head;
+        const int shift = x.HEADS - x.head;
 #pragma unroll
         for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
             const int j = tid + i * THREADS, at = j < k ? record.index[j] : -1;
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIEC
         held.each(x, [&](float (&v)[PIECE<T>], int piece) {
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
-            if (TAIL) add_piece(v, piece_marks<T>(marks, piece, tid), kept, others);
+            if (TAIL) add_piece(v, piece_marks<T, THREADS>(marks, piece, tid), kept, others);
             else others += sum_of(v);
         });
         others = group_sum<THREADS>(others, box);
@@ -244,9 +246,9 @@ __global__ __launch_bounds__(PART_THREADS, 6) void distill_part_kernel(const Dis
         Held<T, PART_THREADS, PART_PIECES> held;
         held.load(x, tid);
         float* const out = (float*)a.workspace + row * split.row_floats(k);
-        const int shift = PIECE<T> - x.head;
+        const int shift = x.HEADS - x.head;
         if (TAIL) {
-            for (int i = tid; i < mark_words(PART_THREADS * PART_PIECES, PIECE<T>); i += PART_THREADS) marks[i] = 0;
+            for (int i = tid; i < mark_words<T, PART_THREADS>(PART_THREADS * PART_PIECES); i += PART_THREADS) marks[i] = 0;
             __syncthreads();
         }
         for (int j = tid; j < k; j += PART_THREADS) {
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(PART_THREADS, 6) void distill_part_kernel(const Dis
         held.each(x, [&](float (&v)[PIECE<T>], int piece) {
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
-            if (TAIL) add_piece(v, piece_marks<T>(marks, piece, tid), kept, others);
+            if (TAIL) add_piece(v, piece_marks<T, PART_THREADS>(marks, piece, tid), kept, others);
             else others += sum_of(v);
         });
         others = group_sum<PART_THREADS>(others, box) * power.off();
@@ -403,7 +405,7 @@ int64_t distill_workspace(int64_t n, int classes, int k, int dtype) {
 
 template <class T, bool TAIL, int THREADS, int PIECES>
 static hipError_t launch_held(const DistillArgs& a, hipStream_t s) {
-    const int lds = 4 * (record_words(a.k) + (TAIL ? mark_words(THREADS * PIECES, PIECE<T>) : 0));
+    const int lds = 4 * (record_words(a.k) + (TAIL ? mark_words<T, THREADS>(THREADS * PIECES) : 0));
     hipLaunchKernelGGL((distill_held_kernel<T, TAIL, THREADS, PIECES>), dim3((unsigned)std::min<int64_t>(a.n, 8192)), dim3(THREADS), lds, s, a);
     return hipGetLastError();
 }
@@ -422,7 +424,7 @@ static hipError_t launch_distill_as(const DistillArgs& a, hipStream_t s) {
     }
     const Parts split = split_rows(a.n, a.classes, a.dtype);
     const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 16)), group(PART_THREADS);
-    const int lds = 4 * (16 + (TAIL ? mark_words(PART_THREADS * PART_PIECES, PIECE<T>) : 0));
+    const int lds = 4 * (16 + (TAIL ? mark_words<T, PART_THREADS>(PART_THREADS * PART_PIECES) : 0));
     hipLaunchKernelGGL((distill_part_kernel<T, TAIL>), grid, group, lds, s, a, split);
     const dim3 joins((unsigned)std::min<int64_t>(a.n * (a.d_logits ? split.parts : 1), 1 << 16));
     hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, true, PART_THREADS, PART_PIECES>), joins, group, 4 * record_words(a.k), s, a, split);

@@ -42,11 +42,11 @@ template <class T, int THREADS, int PIECES>
 __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const RoutedArgs a) {
     __shared__ float box[16];
     const int tid = threadIdx.x, lane = tid & 63, classes = a.classes;
-    const int one = Span<T, THREADS, PIECES>::single(classes, tid);
+    const Uncut<PIECE<T>> cut(classes);                          // (cut in lines of the output there were too few registers: 61 us became 75)
+    const int one = cut.single(tid);
     const bool past = a.n * classes >= 16 << 20;                 // 64 MiB: smaller outputs are in the caches for what reads them next
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         Choices choices(a, row, lane);
-        choices.clear_state(a, row, tid);
         float y[PIECES][PIECE<T>], y_one = 0.f;
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
@@ -57,15 +57,15 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
             const uint64_t same = choices.of(m);
             choices.left &= ~same;
             Span<T, THREADS, PIECES> z;
-            z.load((const T*)a.logits[m] + row * a.ld, classes, tid);
+            z.load((const T*)a.logits[m] + row * a.ld, cut, tid);
             float mx = fmaxf(LOWEST, z.one), sum = 0.f;
-            z.each(classes, [&](const float (&v)[PIECE<T>], int) {
+            z.each(cut, [&](const float (&v)[PIECE<T>], int) {
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) mx = fmaxf(mx, v[e]);
             });
             mx = group_max<THREADS>(mx, box);
             const Exp power(mx, 1.f);
-            z.each(classes, [&](float (&v)[PIECE<T>], int) {
+            z.each(cut, [&](float (&v)[PIECE<T>], int) {
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
                 sum += sum_of(v);
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
             }
             const float share = sum == 0.f ? 0.f : choices.sum(same) / sum;
             y_one = fmaf(share, e_one, y_one);
-            z.each(classes, [&](const float (&v)[PIECE<T>], int i) {
+            z.each(cut, [&](const float (&v)[PIECE<T>], int i) {
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) y[i][e] = fmaf(share, power(v[e]), y[i][e]);
             });
@@ -87,7 +87,8 @@ __global__ __launch_bounds__(THREADS, 4) void combine_routed_kernel(const Routed
         if (one >= 0) out[one] = y_one;
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
-            if (tid < classes / PIECE<T> - i * THREADS) store_floats(out + (i * THREADS + tid) * PIECE<T>, y[i], past);
+            if (tid < cut.pieces - i * THREADS) store_floats(out + cut.head + (i * THREADS + tid) * PIECE<T>, y[i], past);
+        choices.clear_state(a, row, tid);
     }
 }
 
@@ -147,16 +148,17 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
     __shared__ float box[16];
     const int tid = threadIdx.x, lane = tid & 63, classes = a.classes;
     const int per_row = BY_MEMBER ? a.members : a.k;
-    const int one = Span<T, THREADS, PIECES>::single(classes, tid), pieces = classes / PIECE<T>;
     auto one_job = [&](const int64_t row, const Choices& choices, const int what) {
         const int m = BY_MEMBER ? what : __builtin_amdgcn_readlane(choices.member, what);
         if (a.d_weights && what == 0 && tid < a.k && choices.member < 0) a.d_weights[row * a.k + tid] = 0.f;
         const uint64_t same = m < 0 ? 0 : choices.of(m);
         T* const out = BY_MEMBER && a.d_logits[m] ? (T*)a.d_logits[m] + row * a.ld_d : nullptr;
+        const Cut<PIECE<T>, THREADS> cut(out ? out : (const T*)a.logits[m < 0 ? 0 : m] + row * a.ld, sizeof(T), classes);
+        const int one = cut.single(tid), pieces = cut.pieces;
         if (!same || (!BY_MEMBER && __builtin_ctzll(same) != what)) {
             if (!out) return;
             if (one >= 0) out[one] = (T)0.f;
-            for (int i = tid; i < pieces; i += THREADS) store_past(out + (int64_t)i * PIECE<T>, make_uint4(0, 0, 0, 0));
+            for (int i = tid; i < pieces; i += THREADS) store_past(out + cut.head + (int64_t)i * PIECE<T>, make_uint4(0, 0, 0, 0));
             return;
         }
         const int j = __builtin_ctzll(same);
@@ -169,14 +171,14 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
         if constexpr (PIECES > 0) {
             Span<T, THREADS, PIECES> z;
             float g[PIECES][PIECE<T>], g_one = one >= 0 ? g_row[one] : 0.f;
-            z.load(z_row, classes, tid);
+            z.load(z_row, cut, tid);
 #pragma unroll
             for (int i = 0; i < PIECES; i++) {
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) g[i][e] = 0.f;
-                if (tid < pieces - i * THREADS) load_floats(g_row + (i * THREADS + tid) * PIECE<T>, g[i]);
+                if (tid < pieces - i * THREADS) load_floats(g_row + cut.head + (i * THREADS + tid) * PIECE<T>, g[i]);
             }
-            z.each(classes, [&](const float (&v)[PIECE<T>], int i) {
+            z.each(cut, [&](const float (&v)[PIECE<T>], int i) {
                 float t[PIECE<T>];
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) t[e] = power(v[e]) * g[i][e];
@@ -186,11 +188,11 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
             if (out) {
                 const float scale = weight * inverse;
                 if (one >= 0) out[one] = (T)(scale * power(z.one) * (g_one - dot));
-                z.each(classes, [&](float (&v)[PIECE<T>], int i) {
+                z.each(cut, [&](float (&v)[PIECE<T>], int i) {
                     if (tid >= pieces - i * THREADS) return;
 #pragma unroll
                     for (int e = 0; e < PIECE<T>; e++) v[e] = scale * power(v[e]) * (g[i][e] - dot);
-                    store_past((char*)(out + i * THREADS * PIECE<T>) + (uint32_t)tid * 16u, pack(v, out));
+                    store_past((char*)(out + cut.head + i * THREADS * PIECE<T>) + (uint32_t)tid * 16u, pack(v, out));
                 });
             }
         } else {
@@ -201,10 +203,10 @@ __global__ __launch_bounds__(THREADS, PIECES == 8 ? 4 : 5) void combine_routed_b
                 }
                 for (int64_t i = tid; i < pieces; i += THREADS) {
                     float v[PIECE<T>], g[PIECE<T>];
-                    unpack(load_loose(z_row + i * PIECE<T>), v, z_row);
-                    load_floats(g_row + i * PIECE<T>, g);
+                    unpack(load_loose(z_row + cut.head + i * PIECE<T>), v, z_row);
+                    load_floats(g_row + cut.head + i * PIECE<T>, g);
 #pragma unroll
-                    for (int e = 0; e < PIECE<T>; e++) f(v[e], g[e], i * PIECE<T> + e);
+                    for (int e = 0; e < PIECE<T>; e++) f(v[e], g[e], cut.head + i * PIECE<T> + e);
                 }
             };
             walk([&](float v, float g, int64_t) { dot = fmaf(power(v), g, dot); });

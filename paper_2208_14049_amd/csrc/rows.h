@@ -107,14 +107,16 @@ __device__ __forceinline__ float lanes_max(float v) { return unordered(lanes_max
 __device__ __forceinline__ float lanes_sum(float v) { return lanes_fold(v, 0.f, [](float x, float y) { return x + y; }); }
 __device__ __forceinline__ int lanes_sum(int v) { return lanes_fold(v, 0, [](int x, int y) { return x + y; }); }
 
-// A row of `len` elements from `p` on, in any alignment to its elements: the elements in front of the first 16-byte boundary and those
-// behind the last whole piece are taken one to a thread, the pieces between them in turn by all.
+// A row of `len` elements from `p` on, in any alignment to its elements: the elements in front of a boundary and those behind the last whole
+// piece are taken one to a thread, the pieces between them in turn by all.  With 128 threads and more the boundary is a cache line's, so that a
+// wavefront's 1 024 bytes are whole lines (rows of odd length otherwise wrote 7 to 19 % more than they hold), with fewer 16 bytes.
 template <class T, int THREADS>
 struct Row {
+    static constexpr int BOUNDARY = THREADS >= 128 ? 128 : 16, HEADS = BOUNDARY / (int)sizeof(T);     // more than elements in front of it
     const T* p;
     int len, head, pieces;
     __device__ __forceinline__ Row(const T* row, int n) : p(row), len(n) {
-        head = (int)((16u - ((unsigned)(uintptr_t)row & 15u)) & 15u) / (int)sizeof(T);
+        head = (int)(-(unsigned)(uintptr_t)row % BOUNDARY) / (int)sizeof(T);
         if (head > n) head = n;
         pieces = (n - head) / PIECE<T>;
     }
@@ -122,8 +124,8 @@ struct Row {
     // The single element of this thread, or -1.
     __device__ __forceinline__ int single(int tid) const {
         if (tid < head) return tid;
-        const int c = head + pieces * PIECE<T> + tid - PIECE<T>;
-        return tid >= PIECE<T> && c < len ? c : -1;
+        const int c = head + pieces * PIECE<T> + tid - HEADS;
+        return tid >= HEADS && c < len ? c : -1;
     }
     // f(value, class) over this thread's share
     template <class F>
@@ -229,40 +231,67 @@ __device__ __forceinline__ void store_few(T* p, const T (&v)[N]) {
     *(Few*)p = f;
 }
 
-// As Held, but every row is cut from its start on, wherever it begins: class (i THREADS + tid) PIECE + e is element e of piece i in all rows, so that
-// rows of several members can be added in registers.  Classes behind the last whole piece are singles, one a thread.
+// As Held for a row that is cut where another one is (the row that is written, or for short rows the first one read), wherever it begins itself: classes of
+// all rows of a kernel are with the same threads, so that rows of several members can be added in registers.
 template <class T, int THREADS, int PIECES>
 struct Span {
     uint4 r[PIECES];
     float one;
-    static __device__ __forceinline__ int single(int len, int tid) { return len / PIECE<T> * PIECE<T> + tid < len ? len / PIECE<T> * PIECE<T> + tid : -1; }
-    __device__ __forceinline__ void load(const T* p, int len, int tid) {
+    // `cut`: the row that sets head, pieces and single
+    template <class C>
+    __device__ __forceinline__ void load(const T* p, const C& cut, int tid) {
         const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
-        const int pieces = len / PIECE<T>;
         const uint32_t mine = (uint32_t)tid * 16u;
 #pragma unroll
         for (int i = 0; i < PIECES; i++) {
-            const char* const at = (const char*)(p + i * THREADS * PIECE<T>);
-            if ((i + 1) * THREADS <= pieces) r[i] = load_loose(at + mine);
+            const char* const at = (const char*)(p + cut.head + i * THREADS * PIECE<T>);
+            if ((i + 1) * THREADS <= cut.pieces) r[i] = load_loose(at + mine);
             else {
                 r[i] = make_uint4(none, none, none, none);
-                if (tid < pieces - i * THREADS) r[i] = load_loose(at + mine);
+                if (tid < cut.pieces - i * THREADS) r[i] = load_loose(at + mine);
             }
         }
-        one = single(len, tid) >= 0 ? up(p[single(len, tid)]) : NONE;
+        const int c = cut.single(tid);
+        one = c >= 0 ? up(p[c]) : NONE;
     }
     // f(values of piece i, i)
-    template <class F>
-    __device__ __forceinline__ void each(int len, F f) {
+    template <class C, class F>
+    __device__ __forceinline__ void each(const C& cut, F f) {
 #pragma unroll
         for (int i = 0; i < PIECES; i++)
-            if (i * THREADS * PIECE<T> < len) {
+            if (i * THREADS < cut.pieces) {
                 float v[PIECE<T>];
                 if (sizeof(T) == 2) renew(r[i]);
                 unpack(r[i], v, (const T*)nullptr);
                 f(v, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
+    }
+};
+// From its start on, without regard to lines.
+template <int N>
+struct Uncut {
+    static constexpr int head = 0;
+    int len, pieces;
+    __device__ __forceinline__ Uncut(int n) : len(n), pieces(n / N) {}
+    __device__ __forceinline__ int single(int tid) const { return pieces * N + tid < len ? pieces * N + tid : -1; }
+};
+// How a row is cut by what is written: elements of `bytes` each to the next cache line, or to 16 bytes where that may leave more than a wavefront's singles,
+// then pieces of N classes.
+template <int N, int THREADS>
+struct Cut {
+    int len, head, pieces, heads;
+    __device__ __forceinline__ Cut(const void* to, int bytes, int n) : len(n) {
+        const unsigned boundary = THREADS >= 128 || bytes == 4 ? 128 : 16;
+        heads = (int)boundary / bytes;
+        head = (int)(-(unsigned)(uintptr_t)to % boundary) / bytes;
+        if (head > n) head = n;
+        pieces = (n - head) / N;
+    }
+    __device__ __forceinline__ int single(int tid) const {
+        if (tid < head) return tid;
+        const int c = head + pieces * N + tid - heads;
+        return tid >= heads && c < len ? c : -1;
     }
 };
 // Stores PIECE<T> floats of a row, `to` at any multiple of 4 bytes.
