@@ -3,6 +3,10 @@
 //   groups of neighbouring members rank by the sum of their one or two best c; members of the best groups stay
 //   the k best c are chosen, the lowest member on equal ones; weight = scale s, or scale s / (sum of the chosen s)
 // x of minus infinity or NaN: not a member of this row.
+//
+// A wavefront takes a row, up to eight neighbouring members a lane.  Bound by vector instructions, k choices one after the other (a maximum over
+// the lanes is six shifted maxima): 32 768 rows of 256 bf16 members, k = 8, 22 us with the counts, 276 vector instructions a row, where the bytes
+// take 4 us; with a bias 38 us, in eight groups 57, without the counts.  The gradient 10 us.
 #include <algorithm>
 
 #include "operators.h"

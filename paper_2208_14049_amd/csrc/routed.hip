@@ -6,6 +6,8 @@
 // Bound by memory: k rows read and one written, and backward k + 1 read and one for each member written.  Rows are in registers from their
 // maximum to the last use of their values, and the sum over members too, so that each is read once.  A wavefront takes a row of up to 256 pieces of 16
 // bytes, a workgroup one of up to 8 192; longer ones are walked in memory, twice.
+// 8 100 rows of 1 000 fp32 classes, three of twelve members: 24 us (5.0 TB/s as calls, at the rate of memory).  1 023 rows of 32 001 bf16, two of four
+// members: 61 us forward (4.3 TB/s), 116 us backward with the gradients of weights and logits (4.5 TB/s; rows of odd length, two at a time a compute unit).
 #include <algorithm>
 
 #include "operators.h"

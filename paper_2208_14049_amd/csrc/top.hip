@@ -7,6 +7,9 @@
 // Where too many values are no smaller than t (equal ones, most of the row masked, the large ones in few lanes), or too few (NaN), the bound is found
 // by halving, over the row in memory.
 // Rows that are longer than that go in parts, each part's best to the workspace, and a second launch chooses among them.
+// Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 31 us (4.8 TB/s).  The softmax's powers add 9 us to them, k = 100 17 more:
+// comparing the 256 maxima, reading the pieces of some 130 lanes again, ranking as many keys, while the compute unit's other row loads (54 us with both).
+// 8 100 rows of 1 000 fp32 classes, k = 5: 11.3 us, 2.9 TB/s.  One row of 128 000: 12.5 us.
 #include <algorithm>
 
 #include "operators.h"

@@ -574,6 +574,40 @@ def test_offsets_beyond_32_bits():
     check_distill(x, index, t, 1.0, True)
 
 
+def test_no_rows():
+    x, i, t = torch.zeros((0, 10), device="cuda"), torch.zeros((0, 2), dtype=torch.int32, device="cuda"), torch.zeros((0, 2), device="cuda")
+    load = torch.ones(10, dtype=torch.int32, device="cuda")
+    assert [o.shape for o in ens.ens_route(x, 2, load=load)] == [(0, 2)] * 2 and (load == 1).all()
+    assert ens.ens_route_backward(x, i, t).shape == (0, 10)
+    probs, state = ens.ens_combine_routed([x, x], i, t)
+    d_w, d_z = ens.ens_combine_routed_backward([x, x], i, t, state, probs)
+    assert probs.shape == (0, 10) and d_w.shape == (0, 2) and d_z[1].shape == (0, 10)
+    assert [o.shape for o in ens.ens_top(x, 2)] == [(0, 2)] * 2
+    loss, state, d = ens.ens_distill(x, i, t, tail=True, gradient=True)
+    assert loss.shape == (0,) and d.shape == (0, 10) and ens.ens_distill_backward(x, i, t, state).shape == (0, 10)
+
+
+def test_two_calls_at_once():
+    """The same operators on two streams beside each other, workspaces among them."""
+    streams, works, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s in range(2):
+        x = torch.randn((40, 150001), generator=gen(s)).to(torch.bfloat16).cuda()
+        index, t = record(40, 150001, 30, gen(10 + s))
+        works.append((x, index, t, step_inputs(20 + s)))
+
+    def calls(x, index, t, inputs):
+        return list(ens.ens_top(x, 30, form="log_softmax")) + list(ens.ens_distill(x, index, t, tail=True, gradient=True)) + one_step(*inputs)
+    want = [[o.clone() for o in calls(*w)] for w in works]
+    torch.cuda.synchronize()
+    for turn in range(3):
+        outs = []
+        for w, s in zip(works, streams):
+            with torch.cuda.stream(s):
+                outs.append(calls(*w))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for o, w in zip(outs, want) for a, b in zip(o, w)), turn
+
+
 def test_python_refusals():
     x = torch.zeros((4, 10), device="cuda")
     i, t = torch.zeros((4, 2), dtype=torch.int32, device="cuda"), torch.zeros((4, 2), device="cuda")
