@@ -19,7 +19,7 @@ namespace ens {
 
 enum { TOP_VALUE = 0, TOP_LOG = 1, TOP_LOG_SOFTMAX = 2 };
 constexpr int TOP_ROOM = 1024, TOP_WAVE_ROOM = 256;     // candidates in LDS
-constexpr int TOP_WAVE_K = 32;                          // for which the 64 lanes of a wavefront are groups enough
+constexpr int TOP_WAVE_K = 48, TOP_PAIR_K = 96;         // for which the lanes of one or two wavefronts are groups enough
 constexpr int JOIN_THREADS = 1024, JOIN_KEYS = 2048;    // keys of a row's parts: 8 for each of 256 groups, so that those of 128 groups have room
 
 __device__ __forceinline__ uint32_t key_of(float v) { return v != v ? 0u : ordered(v + 0.f); }      // both zeros are one
@@ -133,11 +133,13 @@ struct TopParts {
     __host__ __device__ int64_t bytes(int64_t n, int k) const { return parts == 1 ? 0 : 8 * (keys(n, k) + n * parts); }
 };
 
-// The k-th largest of the maxima of `groups` groups of lanes, as a bound: `own` is the largest of this thread's values.  A group is up to eight
-// neighbouring lanes, which share its comparisons.  *bound is 0 before.
-template <int THREADS>
-__device__ __forceinline__ float find_bound(float own, int groups, int k, float* maxima, uint32_t* bound) {
-    const int tid = threadIdx.x, member = THREADS / groups, some = groups / member;
+// The k-th largest of the maxima of `groups` groups of lanes, as a bound (t): `own` is the largest of this thread's values.  A group is up to eight
+// neighbouring lanes, which share its comparisons.  *bound is 0 before.  LSE: also the row's maximum and its sum of powers, of which powers(Exp) is
+// this thread's share, between the same two barriers.
+struct Bound { float t, mx, sum; };
+template <int THREADS, bool LSE, class F>
+__device__ __forceinline__ Bound find_bound(float own, int groups, int k, float scale, float* maxima, uint32_t* bound, float* box, F powers) {
+    const int tid = threadIdx.x, lane = tid & 63, member = THREADS / groups, some = groups / member;
     float folded = own;
     for (int o = 1; o < member; o <<= 1) folded = fmaxf(folded, __shfl_xor(folded, o, 64));
     if (tid % member == 0) maxima[tid / member] = folded;
@@ -153,9 +155,26 @@ __device__ __forceinline__ float find_bound(float own, int groups, int k, float*
     }
     for (int o = 1; o < member; o <<= 1) no_smaller += __shfl_xor(no_smaller, o, 64);
     const float reached = lanes_max(no_smaller >= k ? folded : LOWEST);      // the largest that k of them reach
-    if ((tid & 63) == 0) atomicMax(bound, key_of(reached));
+    if (lane == 0) atomicMax(bound, key_of(reached));
+    Bound found{0.f, LOWEST, 0.f};
+    float off = 1.f;
+    if (LSE) {
+        for (int i = lane; i < groups; i += 64) found.mx = fmaxf(found.mx, maxima[i]);
+        found.mx = lanes_max(found.mx);
+        const Exp power(found.mx, scale);
+        off = power.off();
+        found.sum = lanes_sum(powers(power));
+        if (lane == 0) box[tid >> 6] = found.sum;
+    }
     group_sync<THREADS>();
-    return value_of(*bound);
+    if (LSE) {
+        found.sum = box[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; w++) found.sum += box[w];
+        found.sum *= off;
+    }
+    found.t = value_of(*bound);
+    return found;
 }
 
 // Short rows for many of their values: fewer pieces of 16 bytes than twice k.  The values are dealt to the threads one by one, so that each has one of the
@@ -180,15 +199,13 @@ __global__ __launch_bounds__(THREADS) void top_dealt_kernel(const TopArgs a) {
             bound = 0;
             count = 0;
         }
-        const float t = find_bound<THREADS>(own, THREADS, k, maxima, &bound);
-        float mx = LOWEST, sum = 0.f;
-        if (LSE) {
-            mx = group_max<THREADS>(own, box);
-            const Exp power(mx, a.inv_temperature);
+        const Bound top = find_bound<THREADS, LSE>(own, THREADS, k, a.inv_temperature, maxima, &bound, box, [&](const Exp& power) {
+            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < EACH; i++) sum += power(v[i]);
-            sum = group_sum<THREADS>(sum, box) * power.off();
-        }
+            return sum;
+        });
+        const float t = top.t, mx = top.mx, sum = top.sum;
 #pragma unroll
         for (int i = 0; i < EACH; i++)
             if (v[i] >= t && tid + i * THREADS < a.classes) {
@@ -223,8 +240,9 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
         const T* const p = (const T*)a.values + row * a.ld + first;
         const Row<T, THREADS> x(p, length);
-        // twice k, so that few values exceed the bound; as many as there are where not all threads have a piece; eight lanes of a group at most
-        const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : max(k <= 32 ? 64 : k <= 64 ? 128 : 256, THREADS / 8);
+        // more than k, so that few values exceed the bound, but with many comparisons of their own (at k = 70 of 128 groups 44 us against 51 of 256, at k = 100
+        // 59 against 57: 3 000 rows of 20 000 fp16); as many as there are where not all threads have a piece; eight lanes of a group at most
+        const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : min(MOST, max(k <= 32 ? 64 : k <= 80 ? 128 : 256, THREADS / 8));
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
         const float own = held.max(x);                           // LOWEST for nothing but minus infinity
@@ -233,19 +251,17 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
             count = 0;
             listed = 0;
         }
-        const float t = find_bound<THREADS>(own, groups, k, maxima, &bound);
-        float mx = LOWEST, sum = 0.f;
-        if (LSE) {
-            mx = group_max<THREADS>(own, box);
-            const Exp power(mx, a.inv_temperature);
+        const Bound top = find_bound<THREADS, LSE>(own, groups, k, a.inv_temperature, maxima, &bound, box, [&](const Exp& power) {
+            float sum = power(held.one);
             held.each(x, [&](const float (&v)[PIECE<T>], int) {
                 float e[PIECE<T>];
 #pragma unroll
                 for (int i = 0; i < PIECE<T>; i++) e[i] = power(v[i]);
                 sum += sum_of(e);
             });
-            sum = group_sum<THREADS>(sum + power(held.one), box) * power.off();
-        }
+            return sum;
+        });
+        const float t = top.t, mx = top.mx, sum = top.sum;
         auto take = [&](float v, int c) {
             if (!(v >= t)) return;
             const int at = atomicAdd(&count, 1);
@@ -425,6 +441,13 @@ static void launch_top_held(const TopArgs& a, const TopParts& split, hipStream_t
     else hipLaunchKernelGGL((top_held_kernel<T, THREADS, PIECES, false>), grid, group, 0, s, a, split);
 }
 
+template <class T, int THREADS>
+static void launch_top_dealt(const TopArgs& a, hipStream_t s) {
+    const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 14)), group(THREADS);
+    if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_dealt_kernel<T, THREADS, 8, true>), rows, group, 0, s, a);
+    else hipLaunchKernelGGL((top_dealt_kernel<T, THREADS, 8, false>), rows, group, 0, s, a);
+}
+
 hipError_t launch_top(const TopArgs& a, hipStream_t s) {
     const TopParts split = split_top(a.classes, a.k, a.dtype);
     return by_type(a.dtype, [&](auto t) {
@@ -436,18 +459,15 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
             return hipGetLastError();
         }
         const int pieces = split.length / PIECE<T>;
-        if (pieces < 2 * a.k && a.classes <= (a.k <= TOP_WAVE_K ? 64 * 8 : 256 * 8)) {
-            const dim3 group(a.k <= TOP_WAVE_K ? 64 : 256);
-            if (a.k <= TOP_WAVE_K) {
-                if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_dealt_kernel<T, 64, 8, true>), rows, group, 0, s, a);
-                else hipLaunchKernelGGL((top_dealt_kernel<T, 64, 8, false>), rows, group, 0, s, a);
-            } else {
-                if (a.form == TOP_LOG_SOFTMAX) hipLaunchKernelGGL((top_dealt_kernel<T, 256, 8, true>), rows, group, 0, s, a);
-                else hipLaunchKernelGGL((top_dealt_kernel<T, 256, 8, false>), rows, group, 0, s, a);
-            }
+        // a wavefront or two take a short row where their lanes are groups enough: 8 100 rows of 1 000 classes for k = 50 took 53 to 60 us with four
+        if (pieces < 2 * a.k && a.classes <= 256 * 8) {
+            if (a.classes <= 64 * 8 && a.k <= TOP_WAVE_K) launch_top_dealt<T, 64>(a, s);
+            else if (a.classes <= 128 * 8 && a.k <= TOP_PAIR_K) launch_top_dealt<T, 128>(a, s);
+            else launch_top_dealt<T, 256>(a, s);
             return hipGetLastError();
         }
         if (pieces <= 64 * 4 && a.k <= TOP_WAVE_K) launch_top_held<T, 64, 4>(a, split, s);
+        else if (pieces <= 128 * 4 && a.k <= TOP_PAIR_K) launch_top_held<T, 128, 4>(a, split, s);
         else if (pieces <= 256 * 4) launch_top_held<T, 256, 4>(a, split, s);
         else if (pieces <= 256 * 16) launch_top_held<T, 256, 16>(a, split, s);
         else if (pieces <= 512 * 16) launch_top_held<T, 512, 16>(a, split, s);

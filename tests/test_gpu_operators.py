@@ -334,7 +334,7 @@ def test_top_orders_and_masks(C, k):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,C,k", [(3, 300, 40), (200, 560, 95), (70, 2047, 128), (5, 100, 30), (2, 263000, 128), (3, 140001, 9), (2, 1100003, 128), (1, 3000001, 5)])
+@pytest.mark.parametrize("n,C,k", [(3, 300, 40), (200, 560, 95), (20, 1000, 70), (33, 700, 48), (20, 1500, 90), (5, 300, 60), (9, 2000, 80), (70, 2047, 128), (5, 100, 30), (2, 263000, 128), (3, 140001, 9), (2, 1100003, 128), (1, 3000001, 5)])
 def test_top_short_and_long(dtype, n, C, k):
     """Rows with fewer 16-byte pieces than twice k, rows in parts, and rows that are too long for them."""
     x = rows(n, C, TYPES[dtype], gen(C + k), 3.0, pad=1)
