@@ -470,11 +470,23 @@ def _row_type(t):
     return code
 
 
+_MOST = (1 << 31) - 1
+
+
+def _kept(k):
+    """k, if a C call takes it."""
+    if not 0 < k <= _MOST:
+        raise ValueError("k is positive, and 32 bits at most")
+    return k
+
+
 def _rows(t, what, dims=2):
     """Shape of a device tensor of rows, and the distance between them."""
     shape = t.shape
     if not t.is_cuda or len(shape) != dims:
         raise ValueError("%s: a device tensor of %d dimensions" % (what, dims))
+    if shape[-1] > _MOST:                                        # a C call takes it in 32 bits
+        raise ValueError("%s: rows of %d elements at most" % (what, _MOST))
     stride = t.stride()
     if shape[-1] > 1 and stride[-1] != 1:
         raise ValueError("%s: the elements of a row stand side by side" % what)
@@ -529,9 +541,9 @@ def _scratch(size, device, where):
 def _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale):
     if score not in _SCORE:
         raise ValueError("score: softmax or sigmoid")
-    if k < 1:
-        raise ValueError("k is positive")
-    return EnsRouteOpts(k, _SCORE[score], groups, groups_kept or groups, group_best, 1 if renormalise else 0, scale)
+    if max(groups, groups_kept or 0, group_best) > _MOST:
+        raise ValueError("groups, groups_kept and group_best: 32 bits at most")
+    return EnsRouteOpts(_kept(k), _SCORE[score], groups, groups_kept or groups, group_best, 1 if renormalise else 0, scale)
 
 
 def ens_route(gates, k, score="softmax", bias=None, groups=1, groups_kept=None, group_best=2, renormalise=True, scale=1.0, load=None):
@@ -580,7 +592,7 @@ def ens_combine_routed(logits, chosen, weights):
     chosen, weights: n x k, as ens_route gives them.  Returns the probabilities (n x classes float32) and the state that the backward pass takes."""
     import torch
     ptrs, one, members, n, classes, ld = _member_rows(logits)
-    k, where = chosen.shape[-1], one.device
+    k, where = _kept(chosen.shape[-1]), one.device
     probs = torch.empty((n, classes), dtype=torch.float32, device=where)
     state = torch.empty((n, k, 2), dtype=torch.float32, device=where)
     _issue(where, "ens_combine_routed", ptrs, _row_type(one), ld, n, members, classes, _plain(chosen, where, (n, k), torch.int32, "chosen"),
@@ -593,7 +605,7 @@ def ens_combine_routed_backward(logits, chosen, weights, state, d_probs, learn=T
     the members learn, or for a list one truth value each; None stands in the place of a gradient that is not wanted."""
     import torch
     ptrs, one, members, n, classes, ld = _member_rows(logits)
-    k, where = chosen.shape[-1], one.device
+    k, where = _kept(chosen.shape[-1]), one.device
     d_weights = torch.empty((n, k), dtype=torch.float32, device=where)
     d_logits, d_ptrs = None, None
     if hasattr(logits, "data_ptr"):
@@ -620,9 +632,7 @@ def ens_top(values, k, form="value", temperature=1.0):
     (n, classes), ld = _rows(values, "values")
     if form not in _FORM:
         raise ValueError("form: value, log or log_softmax")
-    if k < 1:
-        raise ValueError("k is positive")
-    dtype, where = _row_type(values), values.device
+    k, dtype, where = _kept(k), _row_type(values), values.device
     size = lib().ens_top_workspace(n, classes, k, dtype)
     keep, work = _scratch(size, where, "ens_top")
     index = torch.empty((n, k), dtype=torch.int32, device=where)
@@ -647,7 +657,7 @@ def ens_distill(logits, index, log_probs, temperature=1.0, tail=False, row_weigh
     logits; then (loss, state, gradient of the sum of row_weights times loss)."""
     import torch
     (n, classes), ld = _rows(logits, "logits")
-    k, dtype, where = index.shape[-1], _row_type(logits), logits.device
+    k, dtype, where = _kept(index.shape[-1]), _row_type(logits), logits.device
     d, ld_d = (None, 0) if gradient is False or gradient is None else _gradient_rows(logits, gradient)
     size = lib().ens_distill_workspace(n, classes, k, dtype)
     keep, work = _scratch(size, where, "ens_distill")
@@ -663,7 +673,7 @@ def ens_distill_backward(logits, index, log_probs, state, d_loss=None, temperatu
     """Gradient of the logits from that of the losses (None: ones), in their type.  out: a tensor to write to, which may be the logits."""
     import torch
     (n, classes), ld = _rows(logits, "logits")
-    k, where = index.shape[-1], logits.device
+    k, where = _kept(index.shape[-1]), logits.device
     d, ld_d = _gradient_rows(logits, out)
     _issue(where, "ens_distill_backward", logits.data_ptr(), _row_type(logits), ld, n, classes, _plain(index, where, (n, k), torch.int32, "index"),
            _plain(log_probs, where, (n, k), torch.float32, "log_probs"), k, temperature, 1 if tail else 0, _plain(state, where, (n, 3), torch.float32, "state"),

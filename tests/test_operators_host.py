@@ -130,3 +130,32 @@ def test_requests_need_a_handle():
     L = ens.lib()
     assert L.ens_predict_top(None, P, 1, 1, P, P) == ens.ENS_E_INVALID
     assert L.ens_predict_routed(None, P, 1, 1, P, P, P) == ens.ENS_E_INVALID
+
+
+class Sizes:
+    """As much of a device tensor as has to be looked at before its elements."""
+    is_cuda, dtype, device = True, None, None
+
+    def __init__(self, *shape):
+        self.shape = shape
+
+    def data_ptr(self):
+        return 0
+
+    def stride(self, at=None):
+        steps = [1]
+        for size in self.shape[:0:-1]:
+            steps.insert(0, steps[0] * size)
+        return tuple(steps) if at is None else steps[at]
+
+
+def test_sizes_beyond_32_bits():
+    """4 294 967 306 classes are not ten."""
+    wide, ten, kept = Sizes(2, (1 << 32) + 10), Sizes(2, 10), Sizes(2, (1 << 32) + 3)
+    for call in (lambda: ens.ens_top(wide, 3), lambda: ens.ens_route(wide, 3), lambda: ens.ens_distill(wide, Sizes(2, 3), Sizes(2, 3)),
+                 lambda: ens.ens_combine_routed([wide, wide], Sizes(2, 1), Sizes(2, 1)), lambda: ens.ens_route_backward(wide, Sizes(2, 1), Sizes(2, 1)),
+                 lambda: ens.ens_top(ten, (1 << 32) + 3), lambda: ens.ens_route(ten, (1 << 32) + 3), lambda: ens.ens_route(ten, 3, groups=(1 << 32) + 1),
+                 lambda: ens.ens_distill(ten, kept, kept), lambda: ens.ens_distill_backward(ten, kept, kept, None),
+                 lambda: ens.ens_combine_routed([ten], kept, kept), lambda: ens.ens_combine_routed_backward([ten], kept, kept, None, None)):
+        with pytest.raises(ValueError, match="at most"):
+            call()
