@@ -108,6 +108,7 @@ int ens_combine_routed_backward(const void* const* logits, int32_t dtype, int64_
 int64_t ens_top_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype) {
     if (n < 0 || classes < 1 || k < 1 || k > classes || !element_bytes(dtype)) return ENS_E_INVALID;
     if (k > TOP_MAX_K || classes > ROW_MAX) return ENS_E_UNSUPPORTED;
+    if (n > 0 && !rows_fit(n, classes, classes)) return ENS_E_INVALID;
     return n ? top_workspace(n, classes, k, dtype) : 0;
 }
 
@@ -130,6 +131,7 @@ int ens_top(const void* values, int32_t dtype, int64_t ld, int64_t n, int32_t cl
 static int distill_sizes(int64_t n, int32_t classes, int32_t k, int32_t dtype) {
     if (n < 0 || classes < 1 || k < 1 || !element_bytes(dtype)) return ENS_E_INVALID;
     if (k > DISTILL_MAX_K || classes > ROW_MAX) return ENS_E_UNSUPPORTED;
+    if (n > 0 && !rows_fit(n, classes, classes)) return ENS_E_INVALID;
     return ENS_OK;
 }
 

@@ -126,6 +126,14 @@ def test_workspaces():
             assert op(workspace_bytes=want - 1, **size) == ens.ENS_E_INVALID
 
 
+@pytest.mark.parametrize("n", [1 << 45, 1 << 60, (1 << 63) - 1])
+def test_workspaces_of_more_rows_than_offsets_name(n):
+    """The sizes of what no buffer holds are refused, not cut off."""
+    L = ens.lib()
+    for f in (L.ens_top_workspace, L.ens_distill_workspace):
+        assert f(n, 1 << 20, 5, 1) == ens.ENS_E_INVALID
+
+
 def test_requests_need_a_handle():
     L = ens.lib()
     assert L.ens_predict_top(None, P, 1, 1, P, P) == ens.ENS_E_INVALID
