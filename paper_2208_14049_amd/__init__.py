@@ -226,8 +226,18 @@ def _need(true, what):
         raise ValueError(what)
 
 
-def _whole(buf):
-    return bool(buf.flags["C_CONTIGUOUS"]) if isinstance(buf, np.ndarray) else buf.is_contiguous()
+def _whole(buf, kind):
+    """Is a buffer contiguous and of that type?"""
+    return str(buf.dtype).split(".")[-1] == kind and bool(buf.flags["C_CONTIGUOUS"] if isinstance(buf, np.ndarray) else buf.is_contiguous())
+
+
+def _settle(*bufs):
+    """One device for the request's device buffers, and what is still to be written, or read where the library writes, done there."""
+    on = {b.device for b in bufs if _is_device(b)}
+    _need(len(on) <= 1, "device buffers of a request are on one device")
+    for b in bufs:
+        if _is_device(b):
+            return _sync_producer(b)
 
 
 def _empty(on_device, beside, shape, kind):
@@ -345,14 +355,14 @@ class Ensemble:
         """The k most probable classes of every image: (index n x k int32, probability n x k fp32), where ens_predict
         would put its probabilities.  out: such a pair to write to."""
         n, images, dev_in = self._request(images)
+        k = _kept(k)
         if out is None:
             out = _empty(dev_in, images, (n, k), "int32"), _empty(dev_in, images, (n, k), "float32")
         for o, kind in zip(out, ("int32", "float32")):
-            _need(tuple(o.shape) == (n, k) and str(o.dtype).endswith(kind) and _whole(o), "out: two contiguous n x k buffers, int32 and float32")
+            _need(tuple(o.shape) == (n, k) and _whole(o, kind), "out: two contiguous n x k buffers, int32 and float32")
         _need(_is_device(out[0]) == _is_device(out[1]), "out: both on the device or both on the host")
+        _settle(images, *out)
         self._set_io(dev_in, _is_device(out[0]))
-        if dev_in:
-            _sync_producer(images)
         _check(lib().ens_predict_top(self._h, _ptr(images), n, k, _ptr(out[0]), _ptr(out[1])), "ens_predict_top")
         return out
 
@@ -362,14 +372,13 @@ class Ensemble:
         n, images, dev_in = self._request(images)
         _need(tuple(chosen.shape) == tuple(weights.shape) and chosen.ndim == 2 and chosen.shape[0] == n, "chosen and weights are n x k")
         for o, kind in ((chosen, "int32"), (weights, "float32")):
-            _need(str(o.dtype).endswith(kind) and _whole(o) and _is_device(o) == dev_in, "chosen: int32, weights: float32, contiguous, beside the images")
+            _need(_whole(o, kind) and _is_device(o) == dev_in, "chosen: int32, weights: float32, contiguous, beside the images")
         if out is None:
             out = _empty(dev_in, images, (n, self.classes), "float32")
-        _need(tuple(out.shape) == (n, self.classes) and str(out.dtype).endswith("float32") and _whole(out), "out: contiguous n x classes float32")
+        _need(tuple(out.shape) == (n, self.classes) and _whole(out, "float32"), "out: contiguous n x classes float32")
+        _settle(images, chosen, weights, out)
         self._set_io(dev_in, _is_device(out))
-        if dev_in:
-            _sync_producer(images)
-        _check(lib().ens_predict_routed(self._h, _ptr(images), n, int(chosen.shape[1]), _ptr(chosen), _ptr(weights), _ptr(out)), "ens_predict_routed")
+        _check(lib().ens_predict_routed(self._h, _ptr(images), n, _kept(int(chosen.shape[1])), _ptr(chosen), _ptr(weights), _ptr(out)), "ens_predict_routed")
         return out
 
     def _request(self, images):
@@ -385,9 +394,8 @@ class Ensemble:
         """Host array, or written to `out` (n x classes float32, host or device)."""
         if out is None:
             out = np.empty((n, self.classes), dtype=np.float32)
-        _need(tuple(out.shape) == (n, self.classes) and str(out.dtype).endswith("float32") and _whole(out), "out: contiguous n x classes float32")
-        if _is_device(out):
-            _sync_producer(out)                                  # what is still to be read or written there
+        _need(tuple(out.shape) == (n, self.classes) and _whole(out, "float32"), "out: contiguous n x classes float32")
+        _settle(out)
         _check(lib().ens_member_logits(self._h, member, n, _ptr(out)), "ens_member_logits")
         return out
 

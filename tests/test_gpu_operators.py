@@ -672,6 +672,27 @@ def test_requests_that_end_in_operators(on_device):
     E.close()
 
 
+def test_requests_wait_for_readers_of_what_they_write():
+    """Images on the host, answers to device tensors that the stream still reads."""
+    nets, blobs, imgs = tiny()
+    E = ens.Ensemble(nets, blobs)
+    x, n, C, M = np.ascontiguousarray(imgs[:7]), 7, E.classes, E.n_members
+    pair = torch.full((n, 3), -5, dtype=torch.int32, device="cuda"), torch.full((n, 3), -5.0, device="cuda")
+    probs = torch.full((n, C), -5.0, device="cuda")
+    every, same = np.tile(np.arange(M, dtype=np.int32), (n, 1)), np.full((n, M), 1.0 / M, np.float32)
+    E.ens_predict(x)
+    for call, outs in ((lambda: E.ens_predict_top(x, 3, out=pair), pair), (lambda: E.ens_predict_routed(x, every, same, out=probs), (probs,))):
+        torch.cuda._sleep(20_000_000)                            # some 10 ms
+        before = [o.clone() for o in outs]
+        call()
+        assert all((b == -5).all() for b in before) and all((o != -5).any() for o in outs)
+    with pytest.raises(ValueError):
+        E.ens_predict_routed(x, every.astype(np.uint32), same)
+    with pytest.raises(ValueError):
+        E.ens_predict_top(x, 3, out=(np.zeros((n, 3), np.uint32), np.zeros((n, 3), np.float32)))
+    E.close()
+
+
 def test_a_student_of_the_ensemble():
     """From images to a student's gradient: a request, its members' logits, a gate, and the operators behind it."""
     nets, blobs, imgs = tiny()
