@@ -233,7 +233,8 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
     __shared__ __align__(16) float maxima[MOST];
     __shared__ float box[16];
     __shared__ uint32_t bound;
-    __shared__ int count, listed, shares[AGAIN ? THREADS : 1];
+    __shared__ int count, listed;
+    __shared__ uint16_t pieces[AGAIN ? ROOM : 1];
     const int tid = threadIdx.x, k = a.k;
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = split.parts == 1 ? job : job / split.parts;
@@ -245,7 +246,16 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : min(MOST, max(k <= 32 ? 64 : k <= 80 ? 128 : 256, THREADS / 8));
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
-        const float own = held.max(x);                           // LOWEST for nothing but minus infinity
+        float own = fmaxf(LOWEST, held.one), most[PIECES];       // LOWEST for nothing but minus infinity
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) most[i] = NONE;
+        held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
+            float m = v[0];
+#pragma unroll
+            for (int e = 1; e < PIECE<T>; e++) m = fmaxf(m, v[e]);
+            if (AGAIN) most[piece / THREADS] = m;
+            own = fmaxf(own, m);
+        });
         if (tid == 0) {
             bound = 0;
             count = 0;
@@ -269,35 +279,30 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         };
         if (held.at >= 0) take(held.one, held.at);
         if constexpr (AGAIN) {
-            // some k threads hold one: a thread for each of such a thread's pieces reads them again, from the cache
-            constexpr int EACH = PIECES, ROUND = THREADS / EACH;
-            if (own >= t) shares[atomicAdd(&listed, 1)] = tid;
+            // some k pieces hold one: listed, and read again from the cache, by a thread each (those of their threads would be nearly all of the row's lines)
+            uint32_t hits = 0;
+#pragma unroll
+            for (int i = 0; i < PIECES; i++) hits |= most[i] >= t ? 1u << i : 0u;
+            if (hits) {
+                int at = atomicAdd(&listed, __popc(hits));
+                for (; hits; hits &= hits - 1, at++)
+                    if (at < ROOM) pieces[at] = (uint16_t)((__ffs(hits) - 1) * THREADS + tid);
+                    else count = ROOM + 1;                       // more than ROOM values then
+            }
             __syncthreads();
-            const int piece = tid % EACH * THREADS;
-            for (int i = tid / EACH; i < listed; i += 4 * ROUND) {
-                uint4 u[4];
-                int at[4];
+            for (int i = tid; i < min(listed, ROOM); i += THREADS) {
+                const int piece = pieces[i];
+                float v[PIECE<T>];
+                unpack(x.body()[piece], v, p);
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int s = i + e * ROUND;
-                    at[e] = s < listed ? piece + shares[s] : x.pieces;
-                    if (at[e] < x.pieces) u[e] = x.body()[at[e]];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (at[e] < x.pieces) {
-                        float v[PIECE<T>];
-                        unpack(u[e], v, p);
-#pragma unroll
-                        for (int j = 0; j < PIECE<T>; j++) take(v[j], x.head + at[e] * PIECE<T> + j);
-                    }
+                for (int j = 0; j < PIECE<T>; j++) take(v[j], x.head + piece * PIECE<T> + j);
             }
         } else {
             held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
-                float most = v[0];
+                float m = v[0];
 #pragma unroll
-                for (int e = 1; e < PIECE<T>; e++) most = fmaxf(most, v[e]);
-                if (!(most >= t) || tid >= x.pieces - piece) return;
+                for (int e = 1; e < PIECE<T>; e++) m = fmaxf(m, v[e]);
+                if (!(m >= t) || tid >= x.pieces - piece) return;
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; e++) take(v[e], x.head + (piece + tid) * PIECE<T> + e);
             });
