@@ -7,8 +7,8 @@
 // Where too many values are no smaller than t (equal ones, most of the row masked, the large ones in few lanes), or too few (NaN), the bound is found
 // by halving, over the row in memory.
 // Rows that are longer than that go in parts, each part's best to the workspace, and a second launch chooses among them.
-// Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 31 us (4.8 TB/s).  The softmax's powers add 9 us to them, k = 100 17 more:
-// comparing the 256 maxima, reading the pieces of some 130 lanes again, ranking as many keys, while the compute unit's other row loads (54 us with both).
+// Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 32 us (4.6 TB/s).  The softmax's powers add 6 us to them, k = 100 10 more:
+// comparing the 256 maxima, reading some 130 pieces again, ranking as many keys, while the compute unit's other row loads (48 us with both).
 // 8 100 rows of 1 000 fp32 classes, k = 5: 11.3 us, 2.9 TB/s.  One row of 128 000: 12.5 us.
 #include <algorithm>
 
@@ -19,7 +19,7 @@ namespace ens {
 
 enum { TOP_VALUE = 0, TOP_LOG = 1, TOP_LOG_SOFTMAX = 2 };
 constexpr int TOP_ROOM = 1024, TOP_WAVE_ROOM = 256;     // candidates in LDS
-constexpr int TOP_WAVE_K = 48, TOP_PAIR_K = 96;         // for which the lanes of one or two wavefronts are groups enough
+constexpr int TOP_WAVE_K = 48, TOP_PAIR_K = 96;         // for which 64 and 128 groups, the lanes of one and two wavefronts, are enough
 constexpr int JOIN_THREADS = 1024, JOIN_KEYS = 2048;    // keys of a row's parts: 8 for each of 256 groups, so that those of 128 groups have room
 
 __device__ __forceinline__ uint32_t key_of(float v) { return v != v ? 0u : ordered(v + 0.f); }      // both zeros are one
@@ -241,9 +241,9 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         const int part = (int)(job - row * split.parts), first = part * split.length, length = min(split.length, a.classes - first);
         const T* const p = (const T*)a.values + row * a.ld + first;
         const Row<T, THREADS> x(p, length);
-        // more than k, so that few values exceed the bound, but with many comparisons of their own (at k = 70 of 128 groups 44 us against 51 of 256, at k = 100
-        // 59 against 57: 3 000 rows of 20 000 fp16); as many as there are where not all threads have a piece; eight lanes of a group at most
-        const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : min(MOST, max(k <= 32 ? 64 : k <= 80 ? 128 : 256, THREADS / 8));
+        // more than k, so that few values exceed the bound, but with many comparisons of their own (at k = 85 of 128 groups 36 us against 39 of 256, at k = 110
+        // 51 against 43: 3 000 rows of 20 000 fp16); as many as there are where not all threads have a piece; eight lanes of a group at most
+        const int groups = THREADS == 64 ? 64 : x.pieces < THREADS ? MOST : min(MOST, max(k <= 32 ? 64 : k <= TOP_PAIR_K ? 128 : 256, THREADS / 8));
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
         float own = fmaxf(LOWEST, held.one), most[PIECES];       // LOWEST for nothing but minus infinity
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(1024) void top_long_kernel(const TopArgs a) {
 }
 
 // How rows are cut; parts 0: too long.  A row that a workgroup's registers hold stays whole, also where there is only one: 128 000 bf16 classes take
-// 12.8 us whole, as a call from Python, and 16 in 32 parts with the second launch; 32 000 take 11.3 and 15.3, and of 64 and 200 rows 11.3 to
+// 12.3 us whole, as a call from Python, and 16 in 32 parts with the second launch; 32 000 take 11.3 and 15.3, and of 64 and 200 rows 11.3 to
 // 20 and 18 to 31.
 static TopParts split_top(int classes, int k, int dtype) {
     const int pieces = classes / (dtype == 0 ? 4 : 8), parts = pieces > 16384 ? (pieces + 8191) / 8192 : 1;
