@@ -8,7 +8,7 @@
 // by halving, over the row in memory.
 // Rows that are longer than that go in parts, each part's best to the workspace, and a second launch chooses among them.
 // Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 32 us (4.6 TB/s).  The softmax's powers add 6 us to them, k = 100 10 more:
-// comparing the 256 maxima, reading some 130 pieces again, ranking as many keys, while the compute unit's other row loads (48 us with both).
+// comparing the 256 maxima, reading some 130 pieces again, ranking as many keys, while the compute unit's other row loads (47 us with both).
 // 8 100 rows of 1 000 fp32 classes, k = 5: 11.3 us, 2.9 TB/s.  One row of 128 000: 12.5 us.
 #include <algorithm>
 
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
         };
         if (held.at >= 0) take(held.one, held.at);
         if constexpr (AGAIN) {
-            // some k pieces hold one: listed, and read again from the cache, by a thread each (those of their threads would be nearly all of the row's lines)
+            // some k pieces hold one: listed, and read again from the cache, a thread a value (all pieces of their threads would be nearly all of the row's lines)
             uint32_t hits = 0;
 #pragma unroll
             for (int i = 0; i < PIECES; i++) hits |= most[i] >= t ? 1u << i : 0u;
@@ -290,12 +290,9 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
                     else count = ROOM + 1;                       // more than ROOM values then
             }
             __syncthreads();
-            for (int i = tid; i < min(listed, ROOM); i += THREADS) {
-                const int piece = pieces[i];
-                float v[PIECE<T>];
-                unpack(x.body()[piece], v, p);
-#pragma unroll
-                for (int j = 0; j < PIECE<T>; j++) take(v[j], x.head + piece * PIECE<T> + j);
+            for (int i = tid; i < min(listed, ROOM) * PIECE<T>; i += THREADS) {
+                const int c = x.head + pieces[i / PIECE<T>] * PIECE<T> + i % PIECE<T>;
+                take(up(p[c]), c);
             }
         } else {
             held.each(x, [&](const float (&v)[PIECE<T>], int piece) {
