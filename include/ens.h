@@ -386,7 +386,8 @@ int64_t ens_top_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype);
  *   tail 1   q = exp(log_probs), and what they leave of 1 (if anything) is one class more, which stands for all
  *            the classes without an entry: loss = temperature^2 * (sum_c q_c ln(q_c / p_c) + q_0 ln(q_0 / p_0)).
  *            Where the student gives the other classes nothing (none is left, or their logits are minus
- *            infinity) the tail counts nothing.
+ *            infinity) the tail counts nothing.  Finite logits count however far below the kept ones they are: mask
+ *            with minus infinity, not with the type's lowest value.
  * A row with no entry of any probability (tail 0), or whose logits are all minus infinity, has loss and gradient 0.
  *   loss     n;  state  n x 3 floats for the backward pass
  *   d_logits rows of dtype, ld_d apart, or NULL: the gradient of sum_i row_weights[i] * loss[i], in the same pass.

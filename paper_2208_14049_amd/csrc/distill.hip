@@ -1,12 +1,15 @@
 // Distillation: a student's logits x against the classes that a teacher kept of a row, with the logarithms t of their probabilities.
 //   p = softmax(x / T);  q = softmax(t) over the kept classes (tail off), or q = e^t and q_0 = max(0, 1 - sum q) for all the others (tail on)
 //   loss = T^2 (sum q ln(q / p) [+ q_0 ln(q_0 / p_0)]),  p_0 = sum of p over the classes that were not kept
-//   dloss/dx_c = T (S p_c - q_c), S = sum q, and with tail (S = sum q + q_0) for a class that was not kept T (S - q_0 / p_0) p_c
-// A class that is listed twice has the sum of its q.  An entry outside the row is not there.  With tail on and p_0 = 0 the tail counts
-// nothing.  A row without a kept class of any probability (tail off), or without a finite logit, counts nothing.
+//   dloss/dx_c = T (S p_c - q_c), S = sum q (+ q_0);  with tail, for a class that was not kept, T (S - q_0 / p_0) p_c
+// A class that is listed twice has the sum of its q.  An entry outside the row is not there.  With tail on and no other class, or all others at minus
+// infinity, the tail counts nothing.  A row without a kept class of any probability (tail off), or without a finite logit, counts nothing.
 //
-// With E the sum of e = e^((x - max) / T) over the kept classes and R over the others, Z = E + R: both are summed for themselves, since R as a
-// difference would lose what a sure student leaves to the others.  (S - q_0 / p_0) / Z is (sum q - q_0 E / R) / Z.
+// With tail the kept classes and the others each have a maximum and a sum of their own, E = sum e^((x - max_E) / T) and R = sum e^((x - max_R) / T): what a sure
+// student leaves to the others is far below what fp32 holds beside the row's maximum, but its logarithm is not, and neither are the shares of the others in it.
+// With odds = ln (E e^(max_E / T)) - ln (R e^(max_R / T)), p of all kept classes 1 / (1 + e^-odds) and p_0 = 1 / (1 + e^odds), nothing is divided by what can vanish:
+//   dloss/dx_c = T (sum q p_0 - q_0 (1 - p_0)) e^((x_c - max_R) / T) / R   for a class that was not kept
+//   ln p_c = (x_c - max_E) / T - ln E + ln (1 - p_0)                       for one that was
 //
 // Bound by memory: a row read, and its gradient written.  A workgroup keeps a row in registers from its maximum through the sums to the gradient, so that
 // it is read once (up to 131 072 classes of 16 bits, half as many of fp32), with as many threads as leave the most rows to a compute unit at a time;
@@ -30,7 +33,10 @@ struct Record {
     float* q;
     float* sums;
 };
-__device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, int lane, const Record& r) {
+// mark(c) marks class c and says whether it was marked; nullptr for kernels without marks.
+template <class F>
+__device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, int lane, const Record& r, F mark) {
+    constexpr bool MARKS = !std::is_same<F, std::nullptr_t>::value;
     const int32_t* const index = a.index + row * a.k;
     const float* const log_probs = a.log_probs + row * a.k;
     int c[KEPT_LANES];
@@ -60,16 +66,24 @@ __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, i
     }
     // does a class come twice?
     bool twice = false;
+    if constexpr (MARKS) {
+        bool again = false;
 #pragma unroll
-    for (int o = 0; o < KEPT_LANES; o++) {
-        const int entries = min(64, a.k - 64 * o);
-        for (int l = 0; l < entries; l++) {
-            const int other = __builtin_amdgcn_readlane(c[o], l);
-            int same = 0;
+        for (int i = 0; i < KEPT_LANES; i++)
+            if (c[i] >= 0) again = mark(c[i]) || again;
+        twice = __ballot(again) != 0;
+    } else {
 #pragma unroll
-            for (int i = 0; i < KEPT_LANES; i++)
-                if (64 * i < a.k) same += __popcll(__ballot(c[i] == other));
-            twice = twice || (same > 1 && other >= 0);
+        for (int o = 0; o < KEPT_LANES; o++) {
+            const int entries = min(64, a.k - 64 * o);
+            for (int l = 0; l < entries; l++) {
+                const int other = __builtin_amdgcn_readlane(c[o], l);
+                int same = 0;
+#pragma unroll
+                for (int i = 0; i < KEPT_LANES; i++)
+                    if (64 * i < a.k) same += __popcll(__ballot(c[i] == other));
+                twice = twice || (same > 1 && other >= 0);
+            }
         }
     }
     float mass = 0.f, entropy = 0.f;
@@ -120,32 +134,98 @@ __device__ __forceinline__ uint32_t piece_marks(const uint32_t* marks, int first
 template <class T, int THREADS>
 static __host__ __device__ int mark_words(int pieces) { return ((pieces + 1) * PIECE<T> + Row<T, THREADS>::HEADS + 31) / 32; }
 
-// e of a piece into the sums over kept classes and others
-template <int N>
-__device__ __forceinline__ void add_piece(const float (&e)[N], uint32_t marked, float& kept, float& others) {
-    if (__builtin_expect(__ballot(marked != 0) == 0, 1)) {
-        others += sum_of(e);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const bool hit = marked >> i & 1;
-        kept += hit ? e[i] : 0.f;
-        others += hit ? 0.f : e[i];
-    }
+// What a row's record and the student's logits of its classes come to: sum of q, q_0, sum of q ln q; max_E and E (with tail).
+struct Kept { float mass, rest, entropy, max, sum; };
+__device__ __forceinline__ Kept kept_of(const Record& r, float max, float sum) { return Kept{r.sums[0], r.sums[1], r.sums[2], max, sum}; }
+// ln of what the kept classes have over what the others have; plus infinity where the others have nothing, minus infinity where the kept ones (or both) have.
+__device__ __forceinline__ float log_odds(const Kept& kept, float mx, float sum, float temperature) {
+    if (kept.sum == 0.f) return NONE;
+    if (sum == 0.f) return -NONE;
+    return 2.f * ((0.5f * kept.max - 0.5f * mx) / temperature) + (logf(kept.sum) - logf(sum));     // (halves: the difference of two fp32 values may not be one)
 }
-
-// What multiplies e in the gradient of a class that was not kept, and of one that was.
+// A row's loss.  mx, sum: max_R and R with tail, otherwise of all classes.  cross: sum of q (x - max) / T over the kept classes, max max_E with tail,
+// otherwise mx.
+template <bool TAIL>
+__device__ __forceinline__ float row_loss(const Kept& kept, float cross, float mx, float sum, float odds, float T) {
+    float shared = kept.entropy - cross, far = 0.f;              // what is multiplied by T^2, and by 2 T
+    if constexpr (TAIL) {
+        const float mass = kept.mass, rest = sum == 0.f ? 0.f : kept.rest;
+        if (kept.sum == 0.f && sum == 0.f) return 0.f;
+        if (rest > 0.f) shared += rest * logf(rest);
+        if (kept.sum == 0.f) return mass != 0.f ? mass * -NONE : T * T * shared;     // p_0 = 1
+        // -ln p_0 = odds + ln (1 + e^-odds), -ln (1 - p_0) = ln (1 + e^-odds), with both signs the other way round where odds are below 0
+        shared += mass * logf(kept.sum) + (mass + rest) * log1pf(expf(-fabsf(odds)));
+        if (sum != 0.f) {
+            const float tilt = odds < 0.f ? -mass : rest;
+            shared += tilt * (logf(kept.sum) - logf(sum));
+            far += tilt * (0.5f * kept.max - 0.5f * mx);
+        }
+    } else {
+        if (sum == 0.f || kept.mass == 0.f) return 0.f;
+        shared += kept.mass * logf(sum);
+    }
+    return T * T * shared + 2.f * T * far;
+}
+// What multiplies e^((x - max) / T) in the gradient of a class that was not kept, and of one that was, whose maximum is max_E if they stand `apart`.
 struct Factors { float other, kept; };
-// kept_share: E / Z, over_others: 1 / R or 0 where R is
-__device__ __forceinline__ Factors factors(float mass, float rest, float inv_total, float kept_share, float over_others, float weight) {
-    const bool with_rest = rest > 0.f && over_others != 0.f;
-    return Factors{weight * (mass * inv_total - (with_rest ? rest * kept_share * over_others : 0.f)),
-                   weight * (mass + (with_rest ? rest : 0.f)) * inv_total};
+template <bool TAIL>
+__device__ __forceinline__ Factors factors(const Kept& kept, float sum, float odds, float weight, bool apart = TAIL) {
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+    if constexpr (!TAIL) return Factors{weight * kept.mass * inverse, weight * kept.mass * inverse};
+    const float less = expf(-fabsf(odds)), large = 1.f / (1.f + less), small = less * large;
+    const float in = odds < 0.f ? small : large, out = odds < 0.f ? large : small;     // 1 - p_0, p_0
+    const float rest = sum == 0.f ? 0.f : kept.rest;
+    const float share = !apart ? out * inverse : kept.sum == 0.f ? 0.f : in / kept.sum;
+    return Factors{weight * (kept.mass * out - rest * in) * inverse, weight * (kept.mass + rest) * share};
 }
+// Odds up to which the backward pass takes p of the kept classes from the others' maximum and sum, as p_0 e^((x - max_R) / T) / R, which takes no other logits: the
+// odds of the state are rounded at their size, to 2^-21 here, and such a p is off by as much of itself.
+constexpr float NEAR_ODDS = 16.f;
 
-// LDS of a workgroup: a float for each of 16 wavefronts, the record, the marks
-static __host__ __device__ int record_words(int k) { return 16 + 2 * k + 3; }
+// LDS of a workgroup: two floats for each of 16 wavefronts, the record, the marks
+static __host__ __device__ int record_words(int k) { return 32 + 2 * k + 3; }
+__device__ __forceinline__ Record record_in(int* lds, int k) { return Record{lds + 32, (float*)lds + 32 + k, (float*)lds + 32 + 2 * k}; }
+// Two reductions between the same barriers.
+template <int THREADS>
+__device__ __forceinline__ void group_max(float& v, float& w, float* box) {
+    v = lanes_max(v);
+    w = lanes_max(w);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            box[threadIdx.x >> 6] = v;
+            box[16 + (threadIdx.x >> 6)] = w;
+        }
+        __syncthreads();
+        v = box[0];
+        w = box[16];
+#pragma unroll
+        for (int i = 1; i < THREADS / 64; i++) {
+            v = fmaxf(v, box[i]);
+            w = fmaxf(w, box[16 + i]);
+        }
+    }
+}
+template <int THREADS>
+__device__ __forceinline__ void group_sum(float& v, float& w, float* box) {
+    v = lanes_sum(v);
+    w = lanes_sum(w);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            box[threadIdx.x >> 6] = v;
+            box[16 + (threadIdx.x >> 6)] = w;
+        }
+        __syncthreads();
+        v = box[0];
+        w = box[16];
+#pragma unroll
+        for (int i = 1; i < THREADS / 64; i++) {
+            v += box[i];
+            w += box[16 + i];
+        }
+    }
+}
 
 // A workgroup a row, the row in registers between its maximum, its sums and its gradient.  The registers that a thread may use are stated by the
 // wavefronts that are to fit: with 169 instead of 126 a compute unit had one row of 50 001 classes at a time instead of two, 108 us instead of 68.
@@ -153,8 +233,9 @@ template <class T, bool TAIL, int THREADS, int PIECES>
 __global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIECES == 8 ? 5 : 6) void distill_held_kernel(const DistillArgs a) {
     extern __shared__ int lds[];
     const int tid = threadIdx.x, k = a.k;
+    constexpr int KEPT = (DISTILL_MAX_K + THREADS - 1) / THREADS;
     float* const box = (float*)lds;
-    const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
+    const Record record = record_in(lds, k);
     uint32_t* const marks = (uint32_t*)lds + record_words(k);
     const float cooling = 1.f / a.temperature;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -162,81 +243,89 @@ __global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIEC
         const Row<T, THREADS> x(p, a.classes);
         Held<T, THREADS, PIECES> held;
         held.load(x, tid);
-        if (TAIL)
-            for (int i = tid; i < mark_words<T, THREADS>(THREADS * PIECES); i += THREADS) marks[i] = 0;
-        if (tid < 64) read_record(a, row, tid, record);
-        group_sync<THREADS>();
-        float at_kept[(DISTILL_MAX_K + THREADS - 1) / THREADS];
         const int shift = x.HEADS - x.head;
+        if constexpr (TAIL) {
+            if (tid < 64) {
+                for (int i = tid; i < mark_words<T, THREADS>(THREADS * PIECES); i += 64) marks[i] = 0;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                read_record(a, row, tid, record, [&](int c) {
+                    const uint32_t bit = 1u << ((c + shift) & 31);
+                    return (atomicOr(&marks[(c + shift) >> 5], bit) & bit) != 0;
+                });
+            }
+        } else if (tid < 64) read_record(a, row, tid, record, nullptr);
+        group_sync<THREADS>();
+        float at_kept[KEPT], mx, most = LOWEST;
 #pragma unroll
-        for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+        for (int i = 0; i < KEPT; i++) {
             const int j = tid + i * THREADS, at = j < k ? record.index[j] : -1;
-            at_kept[i] = at >= 0 ? up(p[at]) : 0.f;
-            if (TAIL && at >= 0) atomicOr(&marks[(at + shift) >> 5], 1u << ((at + shift) & 31));
+            at_kept[i] = at >= 0 ? up(p[at]) : NONE;
         }
-        const float mx = group_max<THREADS>(held.max(x), box);
-        if (TAIL && THREADS == 64) group_sync<THREADS>();
-        const Exp power(mx, cooling);
-        float kept = 0.f, others = 0.f;
-        {
-            const float e = power(held.one);
-            const bool hit = TAIL && held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1);
-            if (hit) kept = e;
-            else others = e;
-        }
-        held.each(x, [&](float (&v)[PIECE<T>], int piece) {
+        if constexpr (TAIL) {
+            held.hide(x, held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1),
+                      [&](int piece) { return piece_marks<T, THREADS>(marks, piece, tid); });
+            mx = held.max(x);
+#pragma unroll
+            for (int i = 0; i < KEPT; i++) most = fmaxf(most, at_kept[i]);
+            group_max<THREADS>(mx, most, box);
+        } else mx = group_max<THREADS>(held.max(x), box);
+        const Exp power(mx, cooling), power_kept(TAIL ? most : mx, cooling);
+        float sum = power(held.one), sum_kept = 0.f;
+        held.each(x, [&](float (&v)[PIECE<T>], int) {
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
-            if (TAIL) add_piece(v, piece_marks<T, THREADS>(marks, piece, tid), kept, others);
-            else others += sum_of(v);
+            sum += sum_of(v);
         });
-        others = group_sum<THREADS>(others, box);
-        if (TAIL) kept = group_sum<THREADS>(kept, box);
-        const float total = others + kept, off = power.off(), ln_total = logf(total * off);
-        float cross = 0.f;                                       // sum q ln p
+        if constexpr (TAIL) {
 #pragma unroll
-        for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+            for (int i = 0; i < KEPT; i++) sum_kept += power_kept(at_kept[i]);
+            group_sum<THREADS>(sum, sum_kept, box);
+        } else sum = group_sum<THREADS>(sum, box);
+        sum *= power.off();
+        const Kept kept = kept_of(record, most, sum_kept * power_kept.off());
+        const float odds = TAIL ? log_odds(kept, mx, sum, a.temperature) : 0.f;
+        float cross = 0.f;
+#pragma unroll
+        for (int i = 0; i < KEPT; i++) {
             const int j = tid + i * THREADS;
-            if (j < k && record.q[j] != 0.f) cross += record.q[j] * ((at_kept[i] - mx) / a.temperature - ln_total);
+            if (j < k && record.q[j] != 0.f) cross += record.q[j] * ((at_kept[i] - power_kept.m) / a.temperature);
         }
         cross = group_sum<THREADS>(cross, box);
-        const float mass = record.sums[0], rest = record.sums[1];
         if (tid == 0) {
-            const float ln_others = TAIL ? logf(others * off) : NONE;
-            float loss = record.sums[2] - cross;
-            if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
-            a.loss[row] = total == 0.f ? 0.f : loss * a.temperature * a.temperature;
+            a.loss[row] = row_loss<TAIL>(kept, cross, mx, sum, odds, a.temperature);
             a.state[row * 3] = mx;
-            a.state[row * 3 + 1] = ln_total;
-            a.state[row * 3 + 2] = ln_others;
+            a.state[row * 3 + 1] = logf(sum);
+            a.state[row * 3 + 2] = odds;
         }
         if (a.d_logits) {
             T* const out = (T*)a.d_logits + row * a.ld_d;
-            const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature, inv_total = 1.f / total;
-            const bool none = weight == 0.f || total == 0.f;
-            const Factors f = factors(mass, TAIL ? rest : 0.f, inv_total, kept * inv_total, others != 0.f ? 1.f / others : 0.f, weight);
-            if (none) held.map(x, tid, out, [&](float) { return 0.f; });
-            else held.map(x, tid, out, [&](float v) { return f.other * power(v); });
+            const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature;
+            const bool none = weight == 0.f || (sum == 0.f && (!TAIL || odds == NONE));
+            const Factors f = factors<TAIL>(kept, sum, odds, weight);
+            const float other = none ? 0.f : f.other * power.off(), own = f.kept * power_kept.off();
+            if (none) held.clear();
+            held.map(x, tid, out, [&](float v) { return other * power(v); });
             group_sync<THREADS>();
             if (!none)
 #pragma unroll
-                for (int i = 0; i < (DISTILL_MAX_K + THREADS - 1) / THREADS; i++) {
+                for (int i = 0; i < KEPT; i++) {
                     const int j = tid + i * THREADS;
-                    if (j < k && record.index[j] >= 0)
-                        out[record.index[j]] = (T)(f.kept * power(at_kept[i]) - weight * record.q[j]);
+                    if (j < k && record.index[j] >= 0) out[record.index[j]] = (T)(own * power_kept(at_kept[i]) - weight * record.q[j]);
                 }
         }
         group_sync<THREADS>();
     }
 }
 
-// The rows in parts, for rows that are too long for a workgroup's registers or too few: first every part's maximum and sums and the logits of the
+// The rows in parts, for rows that are too long for a workgroup's registers or too few: first every part's maximum and sum and the logits of the
 // kept classes go to the workspace, then every part's workgroup joins them and writes its part of the gradient, the first one the loss.  The second
-// step by itself, from the state, is the backward pass.  A part is in registers too.
+// step by itself, from the state, is the backward pass; where that writes over the logits of several parts, the kept classes wait for a launch of their own, since
+// with tail every one of them needs the logits of all.  A part is in registers too.
 constexpr int PART_THREADS = 256, PART_PIECES = 8;
 struct Parts {
     int parts, length;                                           // of every part but the last
-    __host__ __device__ int64_t row_floats(int k) const { return (int64_t)parts * 3 + k; }
+    bool kept_later;
+    __host__ __device__ int64_t row_floats(int k) const { return (int64_t)parts * 4 + k; }     // maximum and sum of all (with tail of the others), of the kept; the kept classes' logits
 };
 
 template <class T, bool TAIL>
@@ -244,7 +333,7 @@ __global__ __launch_bounds__(PART_THREADS, 6) void distill_part_kernel(const Dis
     extern __shared__ int lds[];
     const int tid = threadIdx.x, k = a.k;
     float* const box = (float*)lds;
-    uint32_t* const marks = (uint32_t*)lds + 16;
+    uint32_t* const marks = (uint32_t*)lds + 32;
     const float cooling = 1.f / a.temperature;
     for (int64_t job = blockIdx.x; job < a.n * split.parts; job += gridDim.x) {
         const int64_t row = job / split.parts;
@@ -259,36 +348,43 @@ __global__ __launch_bounds__(PART_THREADS, 6) void distill_part_kernel(const Dis
             for (int i = tid; i < mark_words<T, PART_THREADS>(PART_THREADS * PART_PIECES); i += PART_THREADS) marks[i] = 0;
             __syncthreads();
         }
-        for (int j = tid; j < k; j += PART_THREADS) {
-            const int64_t at = (int64_t)a.index[row * k + j] - first;
-            if (at < 0 || at >= length) continue;
-            out[split.parts * 3 + j] = up(p[at]);
-            if (TAIL) atomicOr(&marks[(at + shift) >> 5], 1u << ((at + shift) & 31));
+        float at_kept = NONE, most = LOWEST, mx;                 // (PART_THREADS entries at most)
+        if (tid < k) {
+            const int64_t at = (int64_t)a.index[row * k + tid] - first;
+            if (at >= 0 && at < length) {
+                const float v = up(p[at]);
+                out[split.parts * 4 + tid] = v;
+                const uint32_t bit = 1u << ((at + shift) & 31);
+                if (TAIL && !(atomicOr(&marks[(at + shift) >> 5], bit) & bit)) at_kept = v;     // a class that comes twice counts once
+            }
         }
-        const float mx = group_max<PART_THREADS>(held.max(x), box);
-        const Exp power(mx, cooling);
-        float kept = 0.f, others = 0.f;
-        {
-            const float e = power(held.one);
-            if (TAIL && held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1)) kept = e;
-            else others = e;
-        }
-        held.each(x, [&](float (&v)[PIECE<T>], int piece) {
+        if constexpr (TAIL) {
+            __syncthreads();
+            held.hide(x, held.at >= 0 && (marks[(held.at + shift) >> 5] >> ((held.at + shift) & 31) & 1),
+                      [&](int piece) { return piece_marks<T, PART_THREADS>(marks, piece, tid); });
+            mx = held.max(x);
+            most = fmaxf(most, at_kept);
+            group_max<PART_THREADS>(mx, most, box);
+        } else mx = group_max<PART_THREADS>(held.max(x), box);
+        const Exp power(mx, cooling), power_kept(most, cooling);
+        float sum = power(held.one), sum_kept = TAIL ? power_kept(at_kept) : 0.f;
+        held.each(x, [&](float (&v)[PIECE<T>], int) {
 #pragma unroll
             for (int e = 0; e < PIECE<T>; e++) v[e] = power(v[e]);
-            if (TAIL) add_piece(v, piece_marks<T, PART_THREADS>(marks, piece, tid), kept, others);
-            else others += sum_of(v);
+            sum += sum_of(v);
         });
-        others = group_sum<PART_THREADS>(others, box) * power.off();
-        if (TAIL) kept = group_sum<PART_THREADS>(kept, box) * power.off();
+        if constexpr (TAIL) group_sum<PART_THREADS>(sum, sum_kept, box);
+        else sum = group_sum<PART_THREADS>(sum, box);
         if (tid == 0) {
-            out[part * 3] = mx;
-            out[part * 3 + 1] = kept;
-            out[part * 3 + 2] = others;
+            out[part * 4] = mx;
+            out[part * 4 + 1] = sum * power.off();
+            out[part * 4 + 2] = most;
+            out[part * 4 + 3] = sum_kept * power_kept.off();
         }
         __syncthreads();
     }
 }
+static_assert(DISTILL_MAX_K <= PART_THREADS, "a thread an entry");
 
 template <class T, bool TAIL, bool JOIN, int THREADS, int PIECES>
 __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const DistillArgs a, const Parts split) {
@@ -296,7 +392,8 @@ __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const Dist
     __shared__ float found[4];
     constexpr int KEPT = (DISTILL_MAX_K + THREADS - 1) / THREADS;
     const int tid = threadIdx.x, lane = tid & 63, k = a.k;
-    const Record record{lds + 16, (float*)lds + 16 + k, (float*)lds + 16 + 2 * k};
+    float* const box = (float*)lds;
+    const Record record = record_in(lds, k);
     const float cooling = 1.f / a.temperature;
     const int per_row = a.d_logits ? split.parts : 1;            // the first part alone has the loss
     for (int64_t job = blockIdx.x; job < a.n * per_row; job += gridDim.x) {
@@ -306,86 +403,133 @@ __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const Dist
         const T* const p = (const T*)a.logits + row * a.ld + first;
         const Row<T, THREADS> x(p, length);
         Held<T, THREADS, PIECES> held;
-        if (a.d_logits) held.load(x, tid);
+        const bool gradient = !JOIN || a.d_logits;
+        if (gradient) held.load(x, tid);
         if (tid < 64) {
-            read_record(a, row, lane, record);
+            read_record(a, row, lane, record, nullptr);
             if (JOIN) {
-                float m = LOWEST, kept = 0.f, others = 0.f;
-                for (int i = lane; i < split.parts; i += 64) m = fmaxf(m, from[i * 3]);
-                m = lanes_max(m);
-                for (int i = lane; i < split.parts; i += 64) {
-                    const Exp power(m, cooling);
-                    const float less = __builtin_amdgcn_exp2f((from[i * 3] - m) * power.c);
-                    kept += from[i * 3 + 1] * less;
-                    others += from[i * 3 + 2] * less;
-                }
-                kept = lanes_sum(kept);
-                others = lanes_sum(others);
-                if (lane == 0) {
-                    found[0] = m;
-                    found[1] = kept + others;
-                    found[2] = kept;
-                    found[3] = others;
+                constexpr int SETS = TAIL ? 2 : 1;
+                float v[4];                                      // as `found` and a part's four floats
+#pragma unroll
+                for (int e = 0; e < 2 * SETS; e++) v[e] = e % 2 ? 0.f : LOWEST;
+                for (int i = lane; i < split.parts; i += 64)
+#pragma unroll
+                    for (int e = 0; e < 2 * SETS; e += 2) v[e] = fmaxf(v[e], from[i * 4 + e]);
+#pragma unroll
+                for (int e = 0; e < 2 * SETS; e += 2) v[e] = lanes_max(v[e]);
+                for (int i = lane; i < split.parts; i += 64)
+#pragma unroll
+                    for (int e = 0; e < 2 * SETS; e += 2)
+                        v[e + 1] += from[i * 4 + e + 1] * __builtin_amdgcn_exp2f((from[i * 4 + e] - v[e]) * Exp(v[e], cooling).c);
+#pragma unroll
+                for (int e = 0; e < 2 * SETS; e += 2) {
+                    v[e + 1] = lanes_sum(v[e + 1]);
+                    if (lane == 0) {
+                        found[e] = v[e];
+                        found[e + 1] = v[e + 1];
+                    }
                 }
                 if (part == 0) {
-                    const float ln_total = logf(kept + others);
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    const float most = TAIL ? v[2] : v[0];
                     float cross = 0.f;
                     for (int j = lane; j < k; j += 64)
-                        if (record.q[j] != 0.f) cross += record.q[j] * ((from[split.parts * 3 + j] - m) / a.temperature - ln_total);
+                        if (record.q[j] != 0.f) cross += record.q[j] * ((from[split.parts * 4 + j] - most) / a.temperature);
                     cross = lanes_sum(cross);
                     if (lane == 0) {
-                        const float rest = record.sums[1], ln_others = TAIL ? logf(others) : NONE;
-                        float loss = record.sums[2] - cross;
-                        if (TAIL && rest > 0.f && others != 0.f) loss += rest * (logf(rest) - (ln_others - ln_total));
-                        a.loss[row] = kept + others == 0.f ? 0.f : loss * a.temperature * a.temperature;
-                        a.state[row * 3] = m;
-                        a.state[row * 3 + 1] = ln_total;
-                        a.state[row * 3 + 2] = ln_others;
+                        const Kept kept = kept_of(record, most, TAIL ? v[3] : 0.f);
+                        const float odds = TAIL ? log_odds(kept, v[0], v[1], a.temperature) : 0.f;
+                        a.loss[row] = row_loss<TAIL>(kept, cross, v[0], v[1], odds, a.temperature);
+                        a.state[row * 3] = v[0];
+                        a.state[row * 3 + 1] = logf(v[1]);
+                        a.state[row * 3 + 2] = odds;
                     }
                 }
             }
         }
         group_sync<THREADS>();
-        if (a.d_logits) {
+        if (gradient) {
             T* const out = (T*)a.d_logits + row * a.ld_d + first;
-            const float mass = record.sums[0], rest = TAIL ? record.sums[1] : 0.f;
             const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature;
-            float mx, total;
-            Factors f;
-            if (JOIN) {
-                mx = found[0];
-                total = found[1];
-                f = factors(mass, rest, 1.f / total, found[2] / total, found[3] != 0.f ? 1.f / found[3] : 0.f, weight);
-            } else {
-                mx = a.state[row * 3];
-                const float ln_total = a.state[row * 3 + 1], ln_others = a.state[row * 3 + 2];
-                total = expf(ln_total);
-                const bool others = TAIL && ln_others > NONE;
-                f = factors(mass, others ? rest : 0.f, 1.f / total, others ? -expm1f(ln_others - ln_total) : 0.f, others ? expf(-ln_others) : 0.f, weight);
-            }
-            const bool none = weight == 0.f || total == 0.f;
-            float at_kept[KEPT];
+            const float mx = JOIN ? found[0] : a.state[row * 3], sum = JOIN ? found[1] : expf(a.state[row * 3 + 1]);
+            float odds = TAIL && !JOIN ? a.state[row * 3 + 2] : 0.f;
+            // other parts' logits are of use for E, as far as they are not gradients by now
+            const bool far = TAIL && !JOIN && !(fabsf(odds) <= NEAR_ODDS), later = far && split.kept_later, all = far && !later;
+            float at_kept[KEPT], most = LOWEST, sum_kept = 0.f;
             int at[KEPT];
 #pragma unroll
             for (int i = 0; i < KEPT; i++) {
-                const int j = tid + i * THREADS;
-                const int64_t here = j < k && record.index[j] >= 0 ? (int64_t)record.index[j] - first : -1;
-                at[i] = here >= 0 && here < length ? (int)here : -1;
-                at_kept[i] = at[i] < 0 ? 0.f : JOIN ? from[split.parts * 3 + j] : up(p[at[i]]);
+                const int j = tid + i * THREADS, c = j < k ? record.index[j] : -1;
+                const int here = c - first;
+                at[i] = c >= 0 && here >= 0 && here < length ? here : -1;
+                at_kept[i] = !(all ? c >= 0 : at[i] >= 0) ? NONE : JOIN ? from[split.parts * 4 + j] : up(p[here]);
+                most = fmaxf(most, at_kept[i]);
             }
-            group_sync<THREADS>();                               // out may be p
-            const Exp power(mx, cooling);
-            const float other = f.other * power.off(), own = f.kept * power.off();
-            if (none) held.map(x, tid, out, [&](float) { return 0.f; });
-            else held.map(x, tid, out, [&](float v) { return other * power(v); });
-            group_sync<THREADS>();
-            if (!none)
+            if (JOIN && TAIL) {
+                most = found[2];
+                sum_kept = found[3];
+            } else if (all) {
+                most = group_max<THREADS>(most, box);
+                const Exp power(most, cooling);
 #pragma unroll
-                for (int i = 0; i < KEPT; i++)
-                    if (at[i] >= 0) out[at[i]] = (T)(own * power(at_kept[i]) - weight * record.q[tid + i * THREADS]);
+                for (int i = 0; i < KEPT; i++) sum_kept += power(at_kept[i]);
+                sum_kept = group_sum<THREADS>(sum_kept, box) * power.off();
+            }
+            const Kept kept = kept_of(record, most, sum_kept);
+            if (TAIL && JOIN) odds = log_odds(kept, mx, sum, a.temperature);
+            const bool none = weight == 0.f || (sum == 0.f && (!TAIL || odds == NONE));
+            const bool apart = TAIL && (JOIN || far);            // the kept classes by max_E and E
+            const Factors f = factors<TAIL>(kept, sum, odds, weight, apart);
+            group_sync<THREADS>();                               // out may be p
+            const Exp power(mx, cooling), power_kept(apart ? most : mx, cooling);
+            const float other = none ? 0.f : f.other * power.off(), own = f.kept * power_kept.off();
+            if (none) held.clear();
+            held.map(x, tid, out, [&](float v) { return other * power(v); });
+            group_sync<THREADS>();
+#pragma unroll
+            for (int i = 0; i < KEPT; i++) {
+                if (at[i] < 0) continue;
+                if (later) out[at[i]] = (T)at_kept[i];           // as it was
+                else if (!none) out[at[i]] = (T)(own * power_kept(at_kept[i]) - weight * record.q[tid + i * THREADS]);
+            }
         }
         group_sync<THREADS>();
+    }
+}
+
+// The kept classes of rows whose other gradients are written and whose odds are far, a wavefront a row.
+template <class T>
+__global__ __launch_bounds__(64) void distill_kept_kernel(const DistillArgs a) {
+    extern __shared__ int lds[];
+    constexpr int KEPT = DISTILL_MAX_K / 64;
+    const Record record = record_in(lds, a.k);
+    const int lane = threadIdx.x;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const float sum = expf(a.state[row * 3 + 1]), odds = a.state[row * 3 + 2];
+        if (fabsf(odds) <= NEAR_ODDS) continue;
+        const T* const p = (const T*)a.logits + row * a.ld;
+        T* const out = (T*)a.d_logits + row * a.ld_d;
+        read_record(a, row, lane, record, nullptr);
+        group_sync<64>();
+        float at_kept[KEPT], most = LOWEST, sum_kept = 0.f;
+        int at[KEPT];
+#pragma unroll
+        for (int i = 0; i < KEPT; i++) {
+            at[i] = lane + 64 * i < a.k ? record.index[lane + 64 * i] : -1;
+            at_kept[i] = at[i] >= 0 ? up(p[at[i]]) : NONE;
+            most = fmaxf(most, at_kept[i]);
+        }
+        const Exp power(lanes_max(most), 1.f / a.temperature);
+#pragma unroll
+        for (int i = 0; i < KEPT; i++) sum_kept += power(at_kept[i]);
+        const Kept kept = kept_of(record, power.m, lanes_sum(sum_kept) * power.off());
+        const float weight = (a.row_weights ? a.row_weights[row] : 1.f) * a.temperature;
+        const bool none = weight == 0.f || (sum == 0.f && odds == NONE);
+        const float own = factors<true>(kept, sum, odds, weight).kept * power.off();
+#pragma unroll
+        for (int i = 0; i < KEPT; i++)
+            if (at[i] >= 0) out[at[i]] = none ? (T)0.f : (T)(own * power(at_kept[i]) - weight * record.q[lane + 64 * i]);
+        group_sync<64>();
     }
 }
 
@@ -393,10 +537,10 @@ __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const Dist
 static Parts split_rows(int64_t n, int classes, int dtype) {
     const int64_t piece = dtype == 0 ? 4 : 8, most = (classes + 4095) / 4096, want = std::max<int64_t>(1, 1024 / n);
     const int parts = (int)std::max<int64_t>((classes / piece + PART_THREADS * PART_PIECES - 1) / (PART_THREADS * PART_PIECES), std::min(most, want));
-    if (parts <= 1) return Parts{1, classes};
+    if (parts <= 1) return Parts{1, classes, false};
     int length = ((classes + parts - 1) / parts + 63) / 64 * 64;
     length = std::min<int>(length, PART_THREADS * PART_PIECES * piece);
-    return Parts{(classes + length - 1) / length, length};
+    return Parts{(classes + length - 1) / length, length, false};
 }
 
 // A row a workgroup holds it: with 512 threads whatever the rows are, with 1 024 (where a compute unit has one such row at a time) from some rows on.
@@ -432,7 +576,7 @@ static hipError_t launch_distill_as(const DistillArgs& a, hipStream_t s) {
     }
     const Parts split = split_rows(a.n, a.classes, a.dtype);
     const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 16)), group(PART_THREADS);
-    const int lds = 4 * (16 + (TAIL ? mark_words<T, PART_THREADS>(PART_THREADS * PART_PIECES) : 0));
+    const int lds = 4 * (32 + (TAIL ? mark_words<T, PART_THREADS>(PART_THREADS * PART_PIECES) : 0));
     hipLaunchKernelGGL((distill_part_kernel<T, TAIL>), grid, group, lds, s, a, split);
     const dim3 joins((unsigned)std::min<int64_t>(a.n * (a.d_logits ? split.parts : 1), 1 << 16));
     hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, true, PART_THREADS, PART_PIECES>), joins, group, 4 * record_words(a.k), s, a, split);
@@ -446,12 +590,15 @@ template <class T, bool TAIL>
 static hipError_t launch_backward_as(const DistillArgs& a, hipStream_t s) {
     if (a.classes / PIECE<T> <= 64 * 4) {                        // a wavefront a row
         const dim3 rows((unsigned)std::min<int64_t>(a.n, 1 << 16));
-        hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, false, 64, 4>), rows, dim3(64), 4 * record_words(a.k), s, a, Parts{1, a.classes});
+        hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, false, 64, 4>), rows, dim3(64), 4 * record_words(a.k), s, a, Parts{1, a.classes, false});
         return hipGetLastError();
     }
-    const Parts split = split_rows(a.n, a.classes, a.dtype);
+    Parts split = split_rows(a.n, a.classes, a.dtype);
+    split.kept_later = TAIL && split.parts > 1 && a.d_logits == a.logits;
     const dim3 grid((unsigned)std::min<int64_t>(a.n * split.parts, 1 << 16));
     hipLaunchKernelGGL((distill_gradient_kernel<T, TAIL, false, PART_THREADS, PART_PIECES>), grid, dim3(PART_THREADS), 4 * record_words(a.k), s, a, split);
+    if (split.kept_later)
+        hipLaunchKernelGGL((distill_kept_kernel<T>), dim3((unsigned)std::min<int64_t>(a.n, 1 << 16)), dim3(64), 4 * record_words(a.k), s, a);
     return hipGetLastError();
 }
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {

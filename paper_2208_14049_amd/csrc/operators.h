@@ -65,7 +65,7 @@ struct DistillArgs {
     const float* log_probs;      // n x k
     const float* row_weights;    // n, or null for ones: what the gradient of a row is multiplied with
     float* loss;                 // n (forward)
-    float* state;                // n x 3: maximum, logarithms of the sums of e^((x - maximum) / T) over all classes and over those not listed
+    float* state;                // n x 3: maximum and logarithm of the sum of e^((x - maximum) / T), of all classes or with tail of those not listed; with tail ln(p of the listed / p of the others)
     void* d_logits;              // or null (forward)
     int64_t ld_d;
     void* workspace;

@@ -154,18 +154,27 @@ struct Held {
     int at;                                                      // class of `one`, or -1
     __device__ __forceinline__ void load(const Row<T, THREADS>& x, int tid) {
         at = x.single(tid);
-        const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
         const uint32_t mine = (uint32_t)tid * 16u;
 #pragma unroll
         for (int i = 0; i < PIECES; i++) {
             const char* const at_i = (const char*)(x.body() + i * THREADS);
             if ((i + 1) * THREADS <= x.pieces) r[i] = *(const uint4*)(at_i + mine);
             else {
-                r[i] = make_uint4(none, none, none, none);
+                r[i] = nothing();
                 if (tid < x.pieces - i * THREADS) r[i] = *(const uint4*)(at_i + mine);
             }
         }
         one = at >= 0 ? up(x.p[at]) : NONE;
+    }
+    // A piece of minus infinity, and a row of it.
+    static __device__ __forceinline__ uint4 nothing() {
+        const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
+        return make_uint4(none, none, none, none);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) r[i] = nothing();
+        one = NONE;
     }
     // f(values of a piece, number of the piece of thread 0) for pieces in reach of the row
     template <class F>
@@ -186,6 +195,29 @@ struct Held {
             for (int e = 0; e < PIECE<T>; e++) m = fmaxf(m, v[e]);
         });
         return m;
+    }
+    // Minus infinity in the places of marked values: `single` for the single one, a bit each that marks(number of the piece of thread 0) has for a piece's, also
+    // for pieces that are not in reach of the row.  The marks of eight pieces are asked for before the first is looked at.
+    template <class F>
+    __device__ __forceinline__ void hide(const Row<T, THREADS>& x, bool single, F marks) {
+        if (single) one = NONE;
+#pragma unroll
+        for (int first = 0; first < PIECES; first += 8) {
+            uint32_t marked[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8 && first + i < PIECES; i++) marked[i / 4] |= marks((first + i) * THREADS) << (i % 4 * 8);
+            if (__ballot((marked[0] | marked[1]) != 0) == 0) continue;
+#pragma unroll
+            for (int i = 0; i < 8 && first + i < PIECES; i++) {
+                const uint32_t m = marked[i / 4] >> (i % 4 * 8) & 0xFFu;
+                if (__ballot(m != 0) == 0) continue;
+                float v[PIECE<T>];
+                unpack(r[first + i], v, x.p);
+#pragma unroll
+                for (int e = 0; e < PIECE<T>; e++) v[e] = m >> e & 1 ? NONE : v[e];
+                r[first + i] = pack(v, x.p);
+            }
+        }
     }
     // dst[class] = f(value), dst may be the row
     template <class F>

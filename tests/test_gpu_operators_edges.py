@@ -1,0 +1,125 @@
+"""The operators on device buffers at the ends of their ranges, against their definitions in 64 bits: students who are sure, masks of the type's
+lowest value.  Tolerances as test_gpu_operators counts them, or as stated."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2208_14049_amd as ens
+from tests import operators_ref as R
+from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, f64, gen, near, record
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------- distillation
+
+def log_sum(z):
+    m = z.max(initial=-INF)
+    return m if m == -INF else m + math.log(np.exp(z - m).sum())
+
+
+def distill(logits, index, log_probs, T, tail):
+    """operators_ref.distill by logarithms alone, which hold where the probabilities themselves are below the smallest number."""
+    n, C = logits.shape
+    loss, grad = np.zeros(n), np.zeros((n, C))
+    for i in range(n):
+        q, listed, q0 = R.teacher(index[i], log_probs[i], C, tail)
+        z = logits[i] / T
+        log_p = z - log_sum(z)
+        on = q > 0
+        loss[i] = (q[on] * (np.log(q[on]) - log_p[on])).sum()
+        grad[i] = q.sum() * np.exp(log_p) - q
+        if tail and q0 > 0:
+            loss[i] += q0 * (math.log(q0) - (log_sum(z[~listed]) - log_sum(z)))
+            grad[i] += q0 * np.exp(log_p)
+            grad[i, ~listed] -= q0 * R.softmax(z[~listed])
+    return T * T * loss, T * grad
+
+
+def all_ways(logits, index, t, T, tail, w):
+    """(loss, gradient) of every way to get them."""
+    loss, state = ens.ens_distill(logits, index, t, temperature=T, tail=tail)
+    yield "two calls", loss, ens.ens_distill_backward(logits, index, t, state, d_loss=w, temperature=T, tail=tail)
+    loss, state, d = ens.ens_distill(logits, index, t, temperature=T, tail=tail, row_weights=w, gradient=True)
+    yield "one call", loss, d
+    yield "state of one call", loss, ens.ens_distill_backward(logits, index, t, state, d_loss=w, temperature=T, tail=tail)
+    there = logits.clone()
+    yield "backward over the logits", loss, ens.ens_distill_backward(there, index, t, state, d_loss=w, temperature=T, tail=tail, out=there)
+    there = logits.clone()
+    loss, state, d = ens.ens_distill(there, index, t, temperature=T, tail=tail, row_weights=w, gradient=there)
+    yield "gradient over the logits", loss, d
+
+
+# lengths for a wavefront, a workgroup, one of many threads (16 bits) or parts, and parts
+LENGTHS = [40, 1000, 9001, 70001, 200003]
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 4.0])
+@pytest.mark.parametrize("gap", [85.0, 90.0, 100.0, 300.0, -90.0, -300.0])
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_tail_of_a_sure_student(C, gap, T):
+    """The kept classes some 87 temperatures above the others and more, where e^-87 is the smallest normal fp32 value; or as far below."""
+    g = gen(C)
+    for dtype in ((torch.float32, torch.bfloat16) if T == 1.0 else (torch.float32,)):
+        x = torch.randn((3, C), generator=g) * 2
+        index, t = (v.cpu() for v in record(3, C, 6, g))
+        # row 0: all of them; row 1: half of them half as far, so that a part of the row has such a class as its maximum; row 2: one
+        x[0, index[0].long()] += gap * T
+        x[1, index[1].long()] += gap * T / 2
+        x[1, index[1, :3].long()] += gap * T / 2
+        x[2, index[2, 0].long()] += gap * T
+        check_distill(x.to(dtype).cuda(), index.cuda(), t.cuda(), T, True, torch.tensor([6.0, 1.0, 0.5]).cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_tail_where_the_lowest_value_masks(C, dtype):
+    """All classes that the teacher did not keep at the type's lowest value: finite, so that the tail counts.  The loss is then q_0 times the distance, and
+    each of these classes has its share of q_0.  A record's q is off by 44 u of itself and as much of 1 (test_gpu_operators), q_0 as much absolutely."""
+    g = gen(C)
+    lowest = torch.finfo(TYPES[dtype]).min
+    index, t = record(3, C, 6, g)
+    x = torch.full((3, C), lowest)
+    for i in range(3):
+        x[i, index[i].cpu().long()] = torch.randn(6, generator=g)
+    x[2, index[2, 0].long().item()] = lowest                     # one of the kept ones as well
+    x = x.to(TYPES[dtype])
+    w = torch.tensor([1.0, 0.5, 2.0])
+    for T in (1.0, 2.0):
+        loss, grad = distill(f64(x), index.cpu().numpy(), f64(t), T, True)
+        grad *= f64(w)[:, None]
+        q0 = np.array([R.teacher(index[i].cpu().numpy(), f64(t[i]), C, True)[2] for i in range(3)])
+        eq = 60 * U
+        share = np.where(np.abs(f64(x) - lowest) == 0, 1.0 / (C - 6), 1.0)
+        for way, got, d in all_ways(x.cuda(), index, t, T, True, w.cuda()):
+            near(got, loss, eq * (1 + 1 / q0) * np.abs(loss) + 1e-4, way)
+            tol = T * f64(w)[:, None] * (eq + (C / 64 + 60) * U) * share
+            near(d, grad, tol + HALF[x.dtype] * (np.abs(grad) + tol) + LEAST[x.dtype], way)
+
+
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_tail_backward_over_the_logits(C):
+    """The gradient in the logits' place is the one beside them, whatever the odds of the kept classes are, to the order of some 256 additions."""
+    g = gen(C + 1)
+    n, k = 9, 8
+    x = torch.randn((n, C), generator=g) * 2
+    index, t = (v.cpu() for v in record(n, C, k, g))
+    x[1, index[1].long()] += 200.0
+    x[2, index[2].long()] -= 200.0
+    x[3, index[3].long()] = -INF                                 # the others have all
+    x[4] = torch.where(torch.zeros(C).scatter(0, index[4].long(), 1.0) > 0, x[4], -INF)       # the kept ones have all
+    x[5] = -INF
+    index[6, 2:] = index[6, 1]                                   # twice, and more
+    x[6, index[6].long()] += 40.0
+    index[7] = -1
+    w = torch.rand((n,), generator=g) + 0.5
+    w[8] = 0.0
+    x, index, t, w = x.cuda(), index.cuda(), t.cuda(), w.cuda()
+    loss, state = ens.ens_distill(x, index, t, tail=True)
+    want = f64(ens.ens_distill_backward(x, index, t, state, d_loss=w, tail=True))
+    assert np.isfinite(want).all()
+    there = x.clone()
+    got = ens.ens_distill_backward(there, index, t, state, d_loss=w, tail=True, out=there)
+    near(got, want, 2.0 ** -18 * np.abs(want) + 256 * U * f64(w)[:, None])
