@@ -141,13 +141,13 @@ __device__ __forceinline__ Kept kept_of(const Record& r, float max, float sum) {
 __device__ __forceinline__ float log_odds(const Kept& kept, float mx, float sum, float temperature) {
     if (kept.sum == 0.f) return NONE;
     if (sum == 0.f) return -NONE;
-    return 2.f * ((0.5f * kept.max - 0.5f * mx) / temperature) + (logf(kept.sum) - logf(sum));     // (halves: the difference of two fp32 values may not be one)
+    return 2.f * ((0.5f * kept.max - 0.5f * mx) / temperature) + (logf(kept.sum) - logf(sum));     // (halves as in row_loss)
 }
-// A row's loss.  mx, sum: max_R and R with tail, otherwise of all classes.  cross: sum of q (x - max) / T over the kept classes, max max_E with tail,
-// otherwise mx.
+// A row's loss.  mx, sum: max_R and R with tail, otherwise of all classes.  cross: sum of q (x / 2 - max / 2) over the kept classes, max max_E with
+// tail, otherwise mx.  Distances are halved, since those of two fp32 values may not be one, and divided by nothing, since they are multiplied by T in the end.
 template <bool TAIL>
 __device__ __forceinline__ float row_loss(const Kept& kept, float cross, float mx, float sum, float odds, float T) {
-    float shared = kept.entropy - cross, far = 0.f;              // what is multiplied by T^2, and by 2 T
+    float shared = kept.entropy, far = -cross;                   // what is multiplied by T^2, and by 2 T
     if constexpr (TAIL) {
         const float mass = kept.mass, rest = sum == 0.f ? 0.f : kept.rest;
         if (kept.sum == 0.f && sum == 0.f) return 0.f;
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 28 ? 3 : PIECES == 16 ? 4 : PIEC
 #pragma unroll
         for (int i = 0; i < KEPT; i++) {
             const int j = tid + i * THREADS;
-            if (j < k && record.q[j] != 0.f) cross += record.q[j] * ((at_kept[i] - power_kept.m) / a.temperature);
+            if (j < k && record.q[j] != 0.f) cross += record.q[j] * (0.5f * at_kept[i] - 0.5f * power_kept.m);
         }
         cross = group_sum<THREADS>(cross, box);
         if (tid == 0) {
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const Dist
                     const float most = TAIL ? v[2] : v[0];
                     float cross = 0.f;
                     for (int j = lane; j < k; j += 64)
-                        if (record.q[j] != 0.f) cross += record.q[j] * ((from[split.parts * 4 + j] - most) / a.temperature);
+                        if (record.q[j] != 0.f) cross += record.q[j] * (0.5f * from[split.parts * 4 + j] - 0.5f * most);
                     cross = lanes_sum(cross);
                     if (lane == 0) {
                         const Kept kept = kept_of(record, most, TAIL ? v[3] : 0.f);

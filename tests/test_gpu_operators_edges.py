@@ -8,7 +8,7 @@ import torch
 
 import paper_2208_14049_amd as ens
 from tests import operators_ref as R
-from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, f64, gen, near, record
+from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, eps, f64, gen, near, record
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +123,21 @@ def test_distill_tail_backward_over_the_logits(C):
     there = x.clone()
     got = ens.ens_distill_backward(there, index, t, state, d_loss=w, tail=True, out=there)
     near(got, want, 2.0 ** -18 * np.abs(want) + 256 * U * f64(w)[:, None])
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_kept_classes_at_the_lowest_value(C, tail):
+    """A logit that fp32 holds, divided by a temperature below 1, is more than fp32 holds; times the squared temperature it is a loss again."""
+    g = gen(C)
+    index, t = record(2, C, 4, g)
+    x = torch.randn((2, C), generator=g)
+    x[0, index[0, 1].long().item()] = torch.finfo(torch.float32).min
+    x[1, index[1].cpu().long()] = -1e38
+    for T in (0.25, 0.5):
+        loss, grad = distill(f64(x), index.cpu().numpy(), f64(t), T, tail)
+        assert np.isfinite(loss).all() and loss.min() > 1e36
+        for way, got, d in all_ways(x.cuda(), index, t, T, tail, None):
+            near(got, loss, 60 * U * loss, way)
+            tol = T * (eps(12 / T, C) + 60 * U) * np.maximum(np.abs(grad), 2.0 / C) * 2
+            near(d, grad, tol, way)
