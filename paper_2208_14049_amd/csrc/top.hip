@@ -27,6 +27,13 @@ __device__ __forceinline__ float value_of(uint32_t key) { return key == 0u ? __u
 // Larger value first, then lower class; no key is 0.
 __device__ __forceinline__ uint64_t key_of(float v, int c) { return (uint64_t)key_of(v) << 32 | (0xFFFFFFFFu - (uint32_t)c); }
 
+// What is written of a value.  Halves: the difference of two fp32 values may not be one, where it is one at the temperature.
+template <bool LSE>
+__device__ __forceinline__ float answer(const TopArgs& a, float v, float mx, float shift) {
+    if constexpr (LSE) return (0.5f * v - 0.5f * mx) * a.inv_temperature * 2.f - shift;
+    return a.form == TOP_LOG ? logf(v) : v;
+}
+
 template <int THREADS>
 __device__ __forceinline__ int group_count(int v, float* box) {
     v = lanes_sum(v);
@@ -219,7 +226,7 @@ __global__ __launch_bounds__(THREADS) void top_dealt_kernel(const TopArgs a) {
         rank_keys<THREADS>(found, have, k, [&](int at, uint64_t key) {
             const float x = value_of((uint32_t)(key >> 32));
             a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-            a.value[row * k + at] = LSE ? (x - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(x) : x;
+            a.value[row * k + at] = answer<LSE>(a, x, mx, shift);
         });
         group_sync<THREADS>();
     }
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(THREADS, PIECES == 16 ? 4 : 6) void top_held_kernel
             rank_keys<THREADS>(found, have, k, [&](int at, uint64_t key) {
                 const float v = value_of((uint32_t)(key >> 32));
                 a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-                a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
+                a.value[row * k + at] = answer<LSE>(a, v, mx, shift);
             });
         } else {
             uint64_t* const out = (uint64_t*)a.workspace + job * k;
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(const TopArgs a,
         rank_keys<JOIN_THREADS>(found, count, k, [&](int at, uint64_t key) {
             const float v = value_of((uint32_t)(key >> 32));
             a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-            a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
+            a.value[row * k + at] = answer<LSE>(a, v, mx, shift);
         });
         __syncthreads();
     }
@@ -415,7 +422,7 @@ __global__ __launch_bounds__(1024) void top_long_kernel(const TopArgs a) {
         rank_keys<1024>(found, have, k, [&](int at, uint64_t key) {
             const float v = value_of((uint32_t)(key >> 32));
             a.index[row * k + at] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-            a.value[row * k + at] = LSE ? (v - mx) * a.inv_temperature - shift : a.form == TOP_LOG ? logf(v) : v;
+            a.value[row * k + at] = answer<LSE>(a, v, mx, shift);
         });
         __syncthreads();
     }

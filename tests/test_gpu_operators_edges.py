@@ -8,7 +8,7 @@ import torch
 
 import paper_2208_14049_amd as ens
 from tests import operators_ref as R
-from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, eps, f64, gen, near, record
+from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, check_top, eps, f64, gen, near, record
 
 pytestmark = pytest.mark.gpu
 
@@ -141,3 +141,15 @@ def test_distill_kept_classes_at_the_lowest_value(C, tail):
             near(got, loss, 60 * U * loss, way)
             tol = T * (eps(12 / T, C) + 60 * U) * np.maximum(np.abs(grad), 2.0 / C) * 2
             near(d, grad, tol, way)
+
+
+# ------------------------------------------------------------------------------------- best classes
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C,k", [(10, 10), (300, 128), (1000, 128), (5000, 100), (200000, 60), (1100003, 128)])
+def test_top_of_values_far_apart(C, k, dtype):
+    """Two values whose difference is more than fp32 holds, at temperatures that bring its logarithm of a softmax back."""
+    x = torch.full((2, C), -2e38)
+    x[:, ::max(1, C // (k // 2))] = 3e38
+    x[1, C // 3] = 1e38
+    check_top(x.to(TYPES[dtype]).cuda(), k, "log_softmax", 4.0)
