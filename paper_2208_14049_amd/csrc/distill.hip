@@ -420,7 +420,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_gradient_kernel(const Dist
                 for (int i = lane; i < split.parts; i += 64)
 #pragma unroll
                     for (int e = 0; e < 2 * SETS; e += 2)
-                        v[e + 1] += from[i * 4 + e + 1] * __builtin_amdgcn_exp2f((from[i * 4 + e] - v[e]) * Exp(v[e], cooling).c);
+                        v[e + 1] += from[i * 4 + e + 1] * Exp(v[e], cooling).less(from[i * 4 + e]);
 #pragma unroll
                 for (int e = 0; e < 2 * SETS; e += 2) {
                     v[e + 1] = lanes_sum(v[e + 1]);

@@ -70,8 +70,8 @@ struct Exp {
     __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, c, -b)); }
     __device__ __forceinline__ float rest() const { return fmaf(m, c, -b); }
     __device__ __forceinline__ float off() const { return __builtin_amdgcn_exp2f(-rest()); }
-    // what takes sums of these terms to sums of those of a larger maximum
-    __device__ __forceinline__ float to(const Exp& larger) const { return __builtin_amdgcn_exp2f(fmaf(m, larger.c, -larger.b) - rest()); }
+    // what takes a sum relative to a smaller maximum to this one: parts leave their sums multiplied by off, so that the difference of the maxima is all
+    __device__ __forceinline__ float less(float smaller) const { return __builtin_amdgcn_exp2f((smaller - m) * c); }
 };
 
 // A whole number in the order of a float that is no NaN, and back.

@@ -356,7 +356,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(const TopArgs a,
             for (int i = lane; i < split.parts; i += 64) mx = fmaxf(mx, from[i].x);
             mx = lanes_max(mx);
             const Exp power(mx, a.inv_temperature);
-            for (int i = lane; i < split.parts; i += 64) sum += from[i].y * __builtin_amdgcn_exp2f((from[i].x - mx) * power.c);
+            for (int i = lane; i < split.parts; i += 64) sum += from[i].y * power.less(from[i].x);
             sum = lanes_sum(sum);
         }
 #pragma unroll
