@@ -318,11 +318,14 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route
             float c[PER], most, gap, apart = __builtin_inff();
             member_ranks<float, PER>(rule, lane, x, c, most);
             if (a.groups > 1) apart = drop_groups<float, PER>(rule, lane, c, (float*)ranks[wave]);
-            // a score is off by some 20 units of 2^-24 of itself, a rank by half a unit of its own more, a sum of two by twice that
-            told = apart > fmaf(most, 0x1p-16f, 0x1p-120f);
+            // A score s = e^d (/ sum) is off by some 20 units of 2^-24 of itself and 2.5 |d| more: d, its product with log2 e and the constant are rounded at their
+            // own sizes.  |d| is -ln s at most, and s (1 - (ln s) / 8) rises with s, so that the largest s + |bias| bounds it for all members.
+            const float slack = most * fmaf(-__builtin_amdgcn_logf(fmaxf(0x1p-126f, fminf(most, 1.f))), 0.0867f, 1.06f);
+            // 256 units between the ranks of two groups, sums of two scores each, 64 between those of two members
+            told = apart > fmaf(slack, 0x1p-16f, 0x1p-120f);
             if (a.bias) {
                 mine = best_members<PER>(a.k, lane, c, gap);
-                told = told && gap > fmaf(most, 0x1p-18f, 0x1p-120f);
+                told = told && gap > fmaf(slack, 0x1p-18f, 0x1p-120f);
             } else {
                 // members of the groups that stay, by value: scores rise with it, as far as they are not too small for 32 bits
                 bool small = false;

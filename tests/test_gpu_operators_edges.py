@@ -1,5 +1,5 @@
 """The operators on device buffers at the ends of their ranges, against their definitions in 64 bits: students who are sure, masks of the type's
-lowest value.  Tolerances as test_gpu_operators counts them, or as stated."""
+lowest value, scores that 32 bits hold badly.  Tolerances as test_gpu_operators counts them, or as stated."""
 import math
 
 import numpy as np
@@ -8,7 +8,7 @@ import torch
 
 import paper_2208_14049_amd as ens
 from tests import operators_ref as R
-from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, check_top, eps, f64, gen, near, record
+from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, check_route, check_top, eps, f64, gen, near, record
 
 pytestmark = pytest.mark.gpu
 
@@ -153,3 +153,41 @@ def test_top_of_values_far_apart(C, k, dtype):
     x[:, ::max(1, C // (k // 2))] = 3e38
     x[1, C // 3] = 1e38
     check_top(x.to(TYPES[dtype]).cuda(), k, "log_softmax", 4.0)
+
+
+# ------------------------------------------------------------------------------------- routing
+
+def pairs_near_the_border():
+    """32 pairs of gate values near -50, and biases, such that the first of a pair ranks higher by 2^-21 of its score, while scores from products rounded to 32 bits
+    rank the second higher by five times as much: such scores are off by up to 56 units of 2^-24 there."""
+    f = np.float32
+    x = (-50 - np.random.RandomState(0).rand(400000) * 0.05).astype(f)
+    with np.errstate(under="ignore"):
+        rounded = np.exp2((x * f(1.44269504088896341)).astype(np.float64)).astype(f).astype(np.float64)
+    s = 1 / (1 + np.exp(-x.astype(np.float64)))
+    order = np.argsort((rounded - s) / s)
+    low, high = order[:32], order[-32:]
+    # the larger score of a pair has no bias
+    gates, bias = np.empty(64, f), np.zeros(64, f)
+    for i, (a, b) in enumerate(zip(low, high)):
+        gates[2 * i], gates[2 * i + 1] = x[a], x[b]
+        more = s[b] + s[a] * 2.0 ** -21 - s[a]                   # the first one's bias less the second one's
+        bias[2 * i], bias[2 * i + 1] = max(more, 0.0), max(-more, 0.0)
+        ranks = s[a] + float(bias[2 * i]), s[b] + float(bias[2 * i + 1])
+        assert 0 < ranks[0] - ranks[1] < 12 * U * s[a]
+        assert (rounded[b] + bias[2 * i + 1]) - (rounded[a] + bias[2 * i]) > 70 * U * s[a]
+    return torch.from_numpy(gates), torch.from_numpy(bias)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_where_32_bits_misplace_scores(score):
+    """Softmax: a member that the bias takes out has the row's maximum."""
+    pair, bias = pairs_near_the_border()
+    gates = torch.full((32, 65), -INF)
+    for i in range(32):
+        gates[i, 2 * i:2 * i + 2] = pair[2 * i:2 * i + 2]
+    if score == "softmax":
+        gates[:, 64] = 0.0
+    bias = torch.cat([bias, torch.tensor([-INF])])
+    check_route(gates.cuda(), 1, score=score, bias=bias.cuda())
+    check_route(gates.cuda(), 2, score=score, bias=bias.cuda())
