@@ -339,7 +339,8 @@ typedef struct {
  *   load     int32 for each member, or NULL: the call adds the number of rows that chose it
  * A gate value of minus infinity or NaN, and a rank that is one, takes the member out of the row;
  * where fewer than k are left the places behind them hold -1 and weight 0.  Plus infinity counts as the
- * largest fp32 value.  Members 512 at most.  Ranks that differ by less than fp32 resolves are told apart in 64 bits. */
+ * largest fp32 value.  Members 512 at most.  Ranks are those of 64-bit arithmetic: scores that are equal there (of sigmoids beyond 37)
+ * are equal ranks.  Without bias and groups members rank by their gate values themselves. */
 int ens_route(const void* gates, int32_t dtype, int64_t ld, int64_t n, int32_t members, const ens_route_opts* opts, const float* bias,
               int32_t* chosen, float* weights, int32_t* load, void* stream);
 /* Gradient of the gate values from d_weights (n x k), that of the weights; the choice and the bias have none.

@@ -1,5 +1,6 @@
 // Routing: a gate's scores choose members for each row, and weigh them.
-//   s = softmax(x) or sigmoid(x) over the members; a member ranks by c = s + bias, or by x where there is no bias (s rises with x)
+//   s = softmax(x) or sigmoid(x) over the members; a member ranks by c = s + bias as 64 bits give it, or by x where there are neither bias nor groups (s rises
+//   with x)
 //   groups of neighbouring members rank by the sum of their one or two best c; members of the best groups stay
 //   the k best c are chosen, the lowest member on equal ones; weight = scale s, or scale s / (sum of the chosen s)
 // x of minus infinity or NaN: not a member of this row.
@@ -327,14 +328,29 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES<PER>, PER <= 4 ? 8 : 4) void route
                 mine = best_members<PER>(a.k, lane, c, gap);
                 told = told && gap > fmaf(slack, 0x1p-18f, 0x1p-120f);
             } else {
-                // members of the groups that stay, by value: scores rise with it, as far as they are not too small for 32 bits
-                bool small = false;
+                // Members of the groups that stay, by value: their scores rise with it.  Scores of different values are different in 64 bits too, but for tiny ones
+                // (0 in 32 bits), values next to 0 (of 2^-18 and more neighbours lie 2^-41 apart, beside a maximum of 105 at most) and sigmoids next to 1 (beyond 20
+                // neighbours differ by less than 16 units).  Equal scores are ties, which 64 bits settle: rows with two such values at least.
+                uint32_t score = ~0u, near = ~0u;                // the least score, and the least |x| but 0 (less one), as whole numbers
+                float far = NONE;
 #pragma unroll
                 for (int j = 0; j < PER; j++) {
-                    small = small || c[j] == 0.f;
                     x[j] = c[j] > NONE ? x[j] : NONE;
+                    score = min(score, __float_as_uint(c[j]));
+                    near = min(near, (__float_as_uint(x[j]) & 0x7FFFFFFFu) - 1u);
+                    far = fmaxf(far, x[j]);
                 }
-                told = told && __ballot(small) == 0;
+                told = told && __ballot(score == 0u) == 0;
+                const bool large = a.score == SCORE_SIGMOID && far > 20.f;
+                if (__ballot(near < __float_as_uint(0x1p-18f) - 1u || large) != 0) {
+                    int near_zero = 0, near_one = 0;
+#pragma unroll
+                    for (int j = 0; j < PER; j++) {
+                        near_zero += __popcll(__ballot(fabsf(x[j]) < 0x1p-18f));
+                        near_one += __popcll(__ballot(large && x[j] > 20.f));
+                    }
+                    told = told && near_zero < 2 && near_one < 2;
+                }
             }
         }
         if (BY_VALUE || !a.bias) mine = best_by_value<T, PER>(a.k, lane, raw, x);

@@ -191,3 +191,21 @@ def test_route_where_32_bits_misplace_scores(score):
     bias = torch.cat([bias, torch.tensor([-INF])])
     check_route(gates.cuda(), 1, score=score, bias=bias.cuda())
     check_route(gates.cuda(), 2, score=score, bias=bias.cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_in_groups_where_scores_are_equal(score, dtype):
+    """Different gate values whose scores 64 bits do not tell apart are ties, whatever the other groups hold."""
+    x = torch.full((6, 64), -3.0) - torch.arange(64) / 64
+    x[0, 16:32] = torch.arange(40, 56).float()                   # sigmoids of 1
+    x[1, 16:32] = torch.arange(16) * 2.0 ** -70                  # sigmoids of a half
+    x[2, 16:32] = torch.tensor([2.0 ** -60, 0.0, -2.0 ** -60, 2.0 ** -66] * 4)
+    x[3, 16:32] = torch.arange(56, 40, -1).float()
+    x[4, 16:32] = torch.arange(16) * 2.0 ** -14
+    x[5, 16:32] = torch.arange(16, 32).float()
+    x = x.to(TYPES[dtype])
+    for k in (1, 3, 16):
+        check_route(x.cuda(), k, score=score, groups=4, groups_kept=1)
+        check_route(x.cuda(), k, score=score, groups=4, groups_kept=1, group_best=1)
+        check_route(x.cuda(), k, score=score, groups=4, groups_kept=2)
