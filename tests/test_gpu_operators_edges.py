@@ -1,5 +1,5 @@
 """The operators on device buffers at the ends of their ranges, against their definitions in 64 bits: students who are sure, masks of the type's
-lowest value, scores that 32 bits hold badly.  Tolerances as test_gpu_operators counts them, or as stated."""
+lowest value, scores that 32 bits hold badly, single rows.  Tolerances as test_gpu_operators counts them, or as stated."""
 import math
 
 import numpy as np
@@ -8,7 +8,7 @@ import torch
 
 import paper_2208_14049_amd as ens
 from tests import operators_ref as R
-from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_distill, check_route, check_top, eps, f64, gen, near, record
+from tests.test_gpu_operators import HALF, INF, LEAST, TYPES, U, check_combine, check_distill, check_route, check_top, eps, f64, gen, near, record, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -141,6 +141,61 @@ def test_distill_kept_classes_at_the_lowest_value(C, tail):
             near(got, loss, 60 * U * loss, way)
             tol = T * (eps(12 / T, C) + 60 * U) * np.maximum(np.abs(grad), 2.0 / C) * 2
             near(d, grad, tol, way)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,k", [(1, 1), (40, 5), (1000, 5), (9001, 30), (20001, 7), (70001, 40), (128000, 64), (200003, 100), (600003, 3)])
+def test_distill_one_row(dtype, C, k, tail):
+    """A row by itself, its gradient weighed."""
+    g = gen(C)
+    x = rows(1, C, TYPES[dtype], g, 2.0, start=1)
+    index, t = record(1, C, k, g)
+    w = torch.tensor([1.5]).cuda()
+    keep = x.clone()
+    check_distill(x, index, t, 1.25, tail, w)                    # leaves the gradient in x
+    assert C == 1 or x.abs().max() > 0
+    loss, state = ens.ens_distill(keep, index, t, temperature=1.25, tail=tail)
+    want = ens.ens_distill_backward(keep, index, t, state, d_loss=w, temperature=1.25, tail=tail)
+    got = ens.ens_distill_backward(keep, index, t, state, d_loss=w, temperature=1.25, tail=tail, out=keep)
+    assert got is keep and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("n,C", [(520, 20001), (7, 32001), (3, 57003)])
+def test_distill_long_fp32_rows(n, C, tail):
+    g = gen(C)
+    logits = rows(n, C, torch.float32, g, 2.0)
+    index, t = record(n, C, 9, g)
+    check_distill(logits, index, t, 1.0, tail, torch.rand((n,), generator=g).cuda() + 0.1)
+
+
+# ------------------------------------------------------------------------------------- combination
+
+@pytest.mark.parametrize("C", [16385, 20001, 32767, 32768])
+def test_combine_long_fp32_rows(C):
+    g = gen(C)
+    logits = torch.randn((3, 4, C), generator=g).mul(2).cuda()
+    chosen = torch.randint(0, 3, (4, 2), generator=g).int().cuda()
+    check_combine(logits, chosen, torch.randn((4, 2), generator=g).cuda())
+
+
+def test_combine_repeats_itself():
+    """The same bits from the same inputs, other ones in between: rows of odd length, two of four members."""
+    g = gen(1)
+    inputs = []
+    for seed in range(2):
+        logits = torch.randn((4, 257, 32001), generator=g).mul(2).to(torch.bfloat16).cuda()
+        chosen = torch.stack([torch.randperm(4, generator=g)[:2] for _ in range(257)]).int().cuda()
+        inputs.append((logits, chosen, torch.rand((257, 2), generator=g).cuda(), torch.randn((257, 32001), generator=g).cuda()))
+
+    def step(logits, chosen, weights, d):
+        probs, state = ens.ens_combine_routed(logits, chosen, weights)
+        return [probs, state] + list(ens.ens_combine_routed_backward(logits, chosen, weights, state, d))
+    want = [[o.clone() for o in step(*i)] for i in inputs]
+    for turn in range(6):
+        got = step(*inputs[turn % 2])
+        assert all(torch.equal(a, b) for a, b in zip(got, want[turn % 2])), turn
 
 
 # ------------------------------------------------------------------------------------- best classes

@@ -167,3 +167,13 @@ def test_sizes_beyond_32_bits():
                  lambda: ens.ens_combine_routed([ten], kept, kept), lambda: ens.ens_combine_routed_backward([ten], kept, kept, None, None)):
         with pytest.raises(ValueError, match="at most"):
             call()
+
+
+@pytest.mark.parametrize("name,op", [("ens_top_workspace", top), ("ens_distill_workspace", distill)])
+def test_workspaces_of_rows_in_parts(name, op):
+    """Too small, missing or not aligned, for a row that is too long for a workgroup."""
+    size = dict(n=1, classes=300000, k=50, dtype=1)
+    want = getattr(ens.lib(), name)(*size.values())
+    assert want > 0
+    for bad in (dict(workspace=None, workspace_bytes=0), dict(workspace=None), dict(workspace=P + 4), dict(workspace_bytes=want - 1), dict(workspace_bytes=-1)):
+        assert op(ld=300000, **size, **bad) == ens.ENS_E_INVALID
