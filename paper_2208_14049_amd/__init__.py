@@ -549,7 +549,7 @@ def _scratch(size, device, where):
 def _route_opts(k, score, groups, groups_kept, group_best, renormalise, scale):
     if score not in _SCORE:
         raise ValueError("score: softmax or sigmoid")
-    if max(groups, groups_kept or 0, group_best) > _MOST:
+    if max(abs(groups), abs(groups_kept or 0), abs(group_best)) > _MOST:
         raise ValueError("groups, groups_kept and group_best: 32 bits at most")
     return EnsRouteOpts(_kept(k), _SCORE[score], groups, groups_kept or groups, group_best, 1 if renormalise else 0, scale)
 

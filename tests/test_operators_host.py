@@ -177,3 +177,10 @@ def test_workspaces_of_rows_in_parts(name, op):
     assert want > 0
     for bad in (dict(workspace=None, workspace_bytes=0), dict(workspace=None), dict(workspace=P + 4), dict(workspace_bytes=want - 1), dict(workspace_bytes=-1)):
         assert op(ld=300000, **size, **bad) == ens.ENS_E_INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(groups=1 - (1 << 32)), dict(groups=2, groups_kept=1 - (1 << 32)), dict(group_best=1 - (1 << 32))], ids=str)
+def test_sizes_below_32_bits(kw):
+    """What the C call would get as 1."""
+    with pytest.raises(ValueError, match="at most"):
+        ens.ens_route(Sizes(2, 10), 3, **kw)
