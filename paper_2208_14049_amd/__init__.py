@@ -240,6 +240,14 @@ def _settle(*bufs):
             return _sync_producer(b)
 
 
+def _wrote(*bufs):
+    """Autograd is told of what was written to a caller's tensors: it refuses a backward pass that needs what they held."""
+    for b in bufs:
+        if hasattr(b, "data_ptr"):
+            import torch
+            torch.autograd.graph.increment_version(b)
+
+
 def _empty(on_device, beside, shape, kind):
     if not on_device:
         return np.empty(shape, dtype=kind)
@@ -364,6 +372,7 @@ class Ensemble:
         _settle(images, *out)
         self._set_io(dev_in, _is_device(out[0]))
         _check(lib().ens_predict_top(self._h, _ptr(images), n, k, _ptr(out[0]), _ptr(out[1])), "ens_predict_top")
+        _wrote(*out)
         return out
 
     def ens_predict_routed(self, images, chosen, weights, out=None):
@@ -379,6 +388,7 @@ class Ensemble:
         _settle(images, chosen, weights, out)
         self._set_io(dev_in, _is_device(out))
         _check(lib().ens_predict_routed(self._h, _ptr(images), n, _kept(int(chosen.shape[1])), _ptr(chosen), _ptr(weights), _ptr(out)), "ens_predict_routed")
+        _wrote(out)
         return out
 
     def _request(self, images):
@@ -397,6 +407,7 @@ class Ensemble:
         _need(tuple(out.shape) == (n, self.classes) and _whole(out, "float32"), "out: contiguous n x classes float32")
         _settle(out)
         _check(lib().ens_member_logits(self._h, member, n, _ptr(out)), "ens_member_logits")
+        _wrote(out)
         return out
 
     def ens_debug_tensor(self, member, tensor, shape_hwc, n_images):
@@ -458,7 +469,8 @@ class Ensemble:
 
 # ---- operators on device tensors -----------------------------------------------------------------
 # Kernels go to torch's current stream of the tensors' device; nothing is waited for.  Rows may be strided, the elements of a row may not.
-# They record nothing for autograd: the backward passes are calls of their own.
+# They record nothing for autograd, also where an input requires a gradient: the backward passes are calls of their own, whose
+# results go on with tensor.backward(gradient).
 
 _SCORE = {"softmax": 0, "sigmoid": 1}
 _FORM = {"value": 0, "log": 1, "log_softmax": 2}
@@ -564,6 +576,8 @@ def ens_route(gates, k, score="softmax", bias=None, groups=1, groups_kept=None, 
     weights = torch.empty((n, k), dtype=torch.float32, device=where)
     _issue(where, "ens_route", gates.data_ptr(), _row_type(gates), ld, n, members, opts, _plain(bias, where, (members,), torch.float32, "bias"),
            chosen.data_ptr(), weights.data_ptr(), _plain(load, where, (members,), torch.int32, "load"))
+    if load is not None:
+        _wrote(load)
     return chosen, weights
 
 
@@ -674,7 +688,11 @@ def ens_distill(logits, index, log_probs, temperature=1.0, tail=False, row_weigh
     _issue(where, "ens_distill", logits.data_ptr(), dtype, ld, n, classes, _plain(index, where, (n, k), torch.int32, "index"),
            _plain(log_probs, where, (n, k), torch.float32, "log_probs"), k, temperature, 1 if tail else 0,
            _plain(row_weights, where, (n,), torch.float32, "row_weights"), loss.data_ptr(), state.data_ptr(), None if d is None else d.data_ptr(), ld_d, work, size)
-    return (loss, state) if d is None else (loss, state, d)
+    if d is None:
+        return loss, state
+    if d is gradient:
+        _wrote(d)
+    return loss, state, d
 
 
 def ens_distill_backward(logits, index, log_probs, state, d_loss=None, temperature=1.0, tail=False, out=None):
@@ -686,6 +704,8 @@ def ens_distill_backward(logits, index, log_probs, state, d_loss=None, temperatu
     _issue(where, "ens_distill_backward", logits.data_ptr(), _row_type(logits), ld, n, classes, _plain(index, where, (n, k), torch.int32, "index"),
            _plain(log_probs, where, (n, k), torch.float32, "log_probs"), k, temperature, 1 if tail else 0, _plain(state, where, (n, 3), torch.float32, "state"),
            _plain(d_loss, where, (n,), torch.float32, "d_loss"), d.data_ptr(), ld_d)
+    if d is out:
+        _wrote(d)
     return d
 
 

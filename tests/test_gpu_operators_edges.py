@@ -264,3 +264,37 @@ def test_route_in_groups_where_scores_are_equal(score, dtype):
         check_route(x.cuda(), k, score=score, groups=4, groups_kept=1)
         check_route(x.cuda(), k, score=score, groups=4, groups_kept=1, group_best=1)
         check_route(x.cuda(), k, score=score, groups=4, groups_kept=2)
+
+
+# ------------------------------------------------------------------------------------- beside autograd
+
+def test_autograd_sees_what_is_written():
+    """A saved tensor that a call wrote over is not taken for what it was."""
+    g = gen(1)
+    x = torch.randn((4, 50), generator=g).cuda().requires_grad_()
+    index, t = record(4, 50, 3, g)
+    for over in (lambda y: ens.ens_distill(y, index, t, gradient=y),
+                 lambda y: ens.ens_distill_backward(y, index, t, ens.ens_distill(y, index, t)[1], out=y)):
+        y = x.exp()                                              # keeps its result for the backward pass
+        over(y.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    load = torch.zeros(50, dtype=torch.int32, device="cuda")
+    before = load._version
+    ens.ens_route(x, 3, load=load)
+    assert load._version > before
+    before = x._version
+    ens.ens_distill(x, index, t, gradient=True)
+    ens.ens_top(x, 3)
+    assert x._version == before                                  # inputs stay what they are
+
+
+def test_gradients_go_on_by_hand():
+    g = gen(2)
+    inputs, weight = torch.randn((20, 8), generator=g).cuda(), torch.randn((8, 6), generator=g).cuda().requires_grad_()
+    gates = inputs @ weight
+    chosen, weights = ens.ens_route(gates, 2)
+    assert not weights.requires_grad
+    d_gates = ens.ens_route_backward(gates, chosen, torch.ones_like(weights) * torch.arange(2.0, device="cuda"))
+    gates.backward(d_gates)
+    near(weight.grad, f64(inputs).T @ f64(d_gates), 40 * U * (np.abs(f64(inputs)).T @ np.abs(f64(d_gates))))
