@@ -144,6 +144,44 @@ def test_distill_kept_classes_at_the_lowest_value(C, tail):
 
 
 @pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_long_records_of_few_classes(C, tail):
+    """256 entries for 30 classes, so that most come again, also in another 64 of the record."""
+    g = gen(C)
+    x = torch.randn((5, C), generator=g) * 2
+    index = torch.randint(0, 30, (5, 256), generator=g).int()
+    index[1] += C - 30
+    index[2, ::3] = -1
+    index[3, 64:] = torch.arange(192).int() % 30                 # the first 64 and the others by themselves
+    t = torch.log_softmax(torch.randn((5, 256), generator=g), 1) - 0.1
+    check_distill(x.cuda(), index.cuda(), t.cuda(), 1.0, tail, torch.rand((5,), generator=g).cuda() + 0.1)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_at_the_limits_of_the_temperature(C, tail):
+    """2^20: p is even, and a loss of T^2 times logarithms below 20 is off by 80 u of that.  2^-20: p is 0 or 1, the loss T times distances, off by 80 u of itself
+    (a class within 20 T of another would move it; the seeds have none that matters: the least distance counts 50 T)."""
+    g = gen(C + 2)
+    x = torch.randn((3, C), generator=g) * 2
+    x[:, 7] = x.max() + 1.0                                      # the maximum, and the others' maximum
+    x[:, 9] = x.max() - 0.5
+    index = torch.stack([torch.randperm(C - 10, generator=g)[:5] + 10 for _ in range(3)]).int()
+    index[1, 0] = 7
+    t = torch.log_softmax(torch.randn((3, 5), generator=g), 1) - 0.2
+    for T in (2.0 ** 20, 2.0 ** -20):
+        loss, grad = distill(f64(x), index.numpy(), f64(t), T, tail)
+        for i in range(3):
+            z = np.sort(f64(x[i])[np.setdiff1d(np.arange(C), index[i].numpy())])[::-1]
+            assert T > 1 or (z[0] - z[1]) / T > 50
+            kept = np.sort(f64(x[i])[index[i].numpy()])[::-1]
+            assert T > 1 or (kept[0] - kept[1]) / T > 50 and abs(kept[0] - z[0]) / T > 50
+        for way, got, d in all_ways(x.cuda(), index.cuda(), t.cuda(), T, tail, None):
+            near(got, loss, 80 * U * (np.abs(loss) + 20 * T * T), way)
+            near(d, grad, 80 * U * T * np.ones((3, 1)), way)
+
+
+@pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("C,k", [(1, 1), (40, 5), (1000, 5), (9001, 30), (20001, 7), (70001, 40), (128000, 64), (200003, 100), (600003, 3)])
 def test_distill_one_row(dtype, C, k, tail):
