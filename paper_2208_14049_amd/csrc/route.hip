@@ -7,7 +7,8 @@
 //
 // A wavefront takes a row, up to eight neighbouring members a lane.  Bound by vector instructions, k choices one after the other (a maximum over
 // the lanes is six shifted maxima): 32 768 rows of 256 bf16 members, k = 8, 22 us with the counts, 276 vector instructions a row, where the bytes
-// take 4 us; with a bias 38 us, in eight groups 57, without the counts.  The gradient 10 us.
+// take 4 us; with a bias 37 us (softmax) to 42 (sigmoid), in eight groups 45 to 49, both 52 to 57, without the counts.  The gradient 10 us.  With a bias or groups the 64
+// registers that leave room for eight wavefronts are too few: 3 to 5 are spilled at 128 members, 15 to 20 at 256.
 #include <algorithm>
 
 #include "operators.h"

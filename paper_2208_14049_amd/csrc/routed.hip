@@ -5,9 +5,12 @@
 //
 // Bound by memory: k rows read and one written, and backward k + 1 read and one for each member written.  Rows are in registers from their
 // maximum to the last use of their values, and the sum over members too, so that each is read once.  A wavefront takes a row of up to 256 pieces of 16
-// bytes, a workgroup one of up to 8 192; longer ones are walked in memory, twice.
-// 8 100 rows of 1 000 fp32 classes, three of twelve members: 24 us (5.0 TB/s as calls, at the rate of memory).  1 023 rows of 32 001 bf16, two of four
-// members: 61 us forward (4.3 TB/s), 116 us backward with the gradients of weights and logits (4.5 TB/s; rows of odd length, two at a time a compute unit).
+// bytes, a workgroup one of up to 8 192 (backward 4 096); longer ones are walked in memory: forward for the maximum, for the sum and class by class, backward twice.
+// 8 100 rows of 1 000 fp32 classes, three of twelve members: 27 us (4.8 TB/s, as calls without a profiler 26: at the rate of memory).  1 023 rows of 32 001 bf16,
+// two of four members: 76 us forward among the backward passes (3.4 TB/s; 66 by itself over four sets of inputs), 116 us backward with the gradients of weights
+// and logits (4.5 TB/s; rows of odd length, two at a time a compute unit).  64 000 classes: 159 and 275 us.  Long ones are far from memory's rate: 2 048 rows of
+// 128 000 1 008 us forward (2.1 TB/s of what has to move, read three times) and 1 005 backward (4.2); one such row, by one workgroup, 70 and 18.
+// The accumulators of 16-bit rows fill the registers: 4 are spilled with 512 threads (backward too), 17 with 1 024.
 #include <algorithm>
 
 #include "operators.h"

@@ -7,9 +7,10 @@
 // Where too many values are no smaller than t (equal ones, most of the row masked, the large ones in few lanes), or too few (NaN), the bound is found
 // by halving, over the row in memory.
 // Rows that are longer than that go in parts, each part's best to the workspace, and a second launch chooses among them.
-// Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 32 us (4.6 TB/s).  The softmax's powers add 6 us to them, k = 100 10 more:
+// Bound by memory where k is small: 1 500 rows of 50 001 16-bit classes for k = 5 take 31 us (4.8 TB/s).  The softmax's powers add 6 us to them, k = 100 10 more:
 // comparing the 256 maxima, reading some 130 pieces again, ranking as many keys, while the compute unit's other row loads (47 us with both).
-// 8 100 rows of 1 000 fp32 classes, k = 5: 11.3 us, 2.9 TB/s.  One row of 128 000: 12.5 us.
+// 8 100 rows of 1 000 fp32 classes, k = 5: 11.3 us, 2.9 TB/s.  One row of 128 000: 12.5 us.  In parts, k = 50: one row of 300 000 18 us, 40 of them 21.
+// With 4 pieces a thread and a wavefront to four, 2 to 23 of 80 registers are spilled (most in 16 bits and four wavefronts).
 #include <algorithm>
 
 #include "operators.h"
