@@ -384,7 +384,7 @@ int64_t ens_top_workspace(int64_t n, int32_t classes, int32_t k, int32_t dtype);
  *            that temperature.  An entry outside 0 .. classes - 1 is not there; a class that comes twice has
  *            the sum of its probabilities.
  *   tail 0   q = softmax of log_probs over the entries;  loss = temperature^2 * sum_c q_c ln(q_c / p_c)
- *   tail 1   q = exp(log_probs), and what they leave of 1 (if anything) is one class more, which stands for all
+ *   tail 1   q = exp(log_probs), and what they leave of 1 (if 2^-21 at least) is one class more, which stands for all
  *            the classes without an entry: loss = temperature^2 * (sum_c q_c ln(q_c / p_c) + q_0 ln(q_0 / p_0)).
  *            Where the student gives the other classes nothing (none is left, or their logits are minus
  *            infinity) the tail counts nothing.  Finite logits count however far below the kept ones they are: mask

@@ -1,5 +1,5 @@
 // Distillation: a student's logits x against the classes that a teacher kept of a row, with the logarithms t of their probabilities.
-//   p = softmax(x / T);  q = softmax(t) over the kept classes (tail off), or q = e^t and q_0 = max(0, 1 - sum q) for all the others (tail on)
+//   p = softmax(x / T);  q = softmax(t) over the kept classes (tail off), or q = e^t and q_0 = 1 - sum q (0 below 2^-21) for all the others (tail on)
 //   loss = T^2 (sum q ln(q / p) [+ q_0 ln(q_0 / p_0)]),  p_0 = sum of p over the classes that were not kept
 //   dloss/dx_c = T (S p_c - q_c), S = sum q (+ q_0);  with tail, for a class that was not kept, T (S - q_0 / p_0) p_c
 // A class that is listed twice has the sum of its q.  An entry outside the row is not there.  With tail on and no other class, or all others at minus
@@ -27,6 +27,10 @@ namespace ens {
 
 constexpr int KEPT_LANES = DISTILL_MAX_K / 64;
 constexpr int CUS = 256;                                         // compute units
+
+// What less than this is left of 1 is not told from the roundings of q and of their sum; the distance of classes at the lowest value, as a mask leaves them, would
+// make it a loss of 1e30.
+constexpr float LEAST_REST = 0x1p-21f;
 
 // The teacher's record of a row in LDS, as a wavefront leaves it: class (or -1) and q of k entries, the sum of q, q_0, and the sum of q ln q.
 struct Record {
@@ -118,7 +122,7 @@ __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, i
     entropy = lanes_sum(entropy);
     if (lane == 0) {
         r.sums[0] = mass;
-        r.sums[1] = a.tail ? fmaxf(0.f, 1.f - mass) : 0.f;
+        r.sums[1] = a.tail && 1.f - mass >= LEAST_REST ? 1.f - mass : 0.f;
         r.sums[2] = entropy;
     }
 }

@@ -125,6 +125,24 @@ def test_distill_tail_backward_over_the_logits(C):
     near(got, want, 2.0 ** -18 * np.abs(want) + 256 * U * f64(w)[:, None])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C", LENGTHS)
+def test_distill_whole_records_where_the_lowest_value_masks(C, dtype):
+    """Entries for all classes that a mask leaves, whose probabilities add up to 1 but for a rounding: the tail is nothing, not that rounding times the distance."""
+    g = gen(C + 3)
+    x = torch.full((4, C), torch.finfo(TYPES[dtype]).min)
+    index = torch.stack([torch.randperm(C, generator=g)[:20] for _ in range(4)]).int()
+    for i in range(4):
+        x[i, index[i].long()] = torch.randn(20, generator=g)
+    x = x.to(TYPES[dtype]).cuda()
+    index, t = index.cuda(), torch.log_softmax(torch.randn((4, 20), generator=g) * 3, 1).cuda()
+    for T in (1.0, 2.0):
+        ways = [list(all_ways(x, index, t, T, tail, None)) for tail in (False, True)]
+        for (way, loss, d), (_, loss_tail, d_tail) in zip(*ways):
+            near(loss_tail, f64(loss), 100 * U * T * T * 20, way)          # logarithms below 20
+            near(d_tail, f64(d), 100 * U * T + 2 * HALF[x.dtype] * np.abs(f64(d)), way)
+
+
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("C", LENGTHS)
 def test_distill_kept_classes_at_the_lowest_value(C, tail):
