@@ -78,18 +78,25 @@ __device__ __forceinline__ void read_record(const DistillArgs& a, int64_t row, i
             if (c[i] >= 0) again = mark(c[i]) || again;
         twice = __ballot(again) != 0;
     } else {
+        int times[KEPT_LANES] = {};                              // that an entry's class comes
+        auto count = [&](auto groups) {
+            constexpr int GROUPS = decltype(groups)::value;
 #pragma unroll
-        for (int o = 0; o < KEPT_LANES; o++) {
-            const int entries = min(64, a.k - 64 * o);
-            for (int l = 0; l < entries; l++) {
-                const int other = __builtin_amdgcn_readlane(c[o], l);
-                int same = 0;
+            for (int o = 0; o < GROUPS; o++) {
+                const int entries = min(64, a.k - 64 * o);
+                for (int l = 0; l < entries; l++) {
+                    const int other = __builtin_amdgcn_readlane(c[o], l);
 #pragma unroll
-                for (int i = 0; i < KEPT_LANES; i++)
-                    if (64 * i < a.k) same += __popcll(__ballot(c[i] == other));
-                twice = twice || (same > 1 && other >= 0);
+                    for (int i = 0; i < GROUPS; i++) times[i] += c[i] == other;
+                }
             }
-        }
+        };
+        if (a.k <= 64) count(std::integral_constant<int, 1>());
+        else count(std::integral_constant<int, KEPT_LANES>());
+        bool again = false;
+#pragma unroll
+        for (int i = 0; i < KEPT_LANES; i++) again = again || (c[i] >= 0 && times[i] > 1);
+        twice = __ballot(again) != 0;
     }
     float mass = 0.f, entropy = 0.f;
 #pragma unroll
