@@ -15,9 +15,9 @@
 // it is read once (up to 131 072 classes of 16 bits, half as many of fp32), with as many threads as leave the most rows to a compute unit at a time;
 // longer rows, and few of the longest, go in parts of 2 048 pieces of 16 bytes, which are read twice.  The teacher's record is read by the first
 // wavefront while the others' loads are on their way.
-// Gradient with the loss, as calls: 4 096 rows of 128 000 bf16 classes 416 us (5.04 TB/s of what has to move; torch's copy of them 400), with the tail 445; 1 021
-// rows of 50 001 with the tail 48 us (4.25 TB/s, two rows a compute unit at a time, whose ends leave it idle); parts: 700 rows of 200 000 160 us, with the tail
-// 167, 2 048 rows of 151 936 347 and 365 (3.5 TB/s, read twice).  Backward by itself 49, 106 and 224 us for the last three (4.2 to 5.5 TB/s).
+// Gradient with the loss, k = 50, as calls: 4 096 rows of 128 000 bf16 classes 423 us (4.96 TB/s of what has to move; torch's copy of them 400), with the tail
+// 447; 1 021 rows of 50 001 47 and 48 us (4.3 TB/s, two rows a compute unit at a time, whose ends leave it idle); in parts, read twice, 700 rows of 200 000 154 and
+// 158, 2 048 rows of 151 936 344 and 349 (3.6 TB/s).  Backward by itself 42, 102 and 225 us for the last three (4.8 to 5.5 TB/s).
 #include <algorithm>
 
 #include "operators.h"
